@@ -10,6 +10,7 @@ Ranges (`listed` and `draw` alike): matrices from 1 x 64 to 11008 x 4096, wide a
 in a call; three to seven steps of the iteration; tensors from one element to about 70 million; bfloat16 and float32
 weights and gradients.  Gradients are noise and 64 (or fewer) strong directions, the momentum is what such gradients leave.
 """
+import functools
 import math
 
 import torch
@@ -123,22 +124,6 @@ def _signal(m, n, gen):
     return 10 * (math.sqrt(m) + math.sqrt(n)) / math.sqrt(n) * (u @ v.T)
 
 
-class _Plans:
-    """The handles that a program keeps, given back with it."""
-
-    def __init__(self, destroy):
-        self.by_key, self.destroy = {}, destroy
-
-    def get(self, key, make):
-        if key not in self.by_key:
-            self.by_key[key] = make()
-        return self.by_key[key]
-
-    def __del__(self):
-        for h in self.by_key.values():
-            self.destroy(h)
-
-
 def prepare(case, seed):
     gen = torch.Generator(device="cuda")
     gen.manual_seed(seed * 1009 + 17)
@@ -167,29 +152,33 @@ def prepare(case, seed):
     return s
 
 
+@functools.cache
+def _adamw_plan(numel, xt, gt):
+    from paper_2605_16341_b200 import binding as od
+    h = od.orthdion_adamw_create(numel, BETA1, BETA2, ADAM_EPS, ADAM_ETA, ADAM_WD)
+    od.orthdion_adamw_set_dtypes(h, xt, gt)
+    return h
+
+
+@functools.cache
+def _muon_plan(m, n, xt, gt, nesterov, poly, steps):
+    from paper_2605_16341_b200 import binding as od
+    h = od.orthdion_muon_create(m, n, MU, ETA, WD, nesterov)
+    od.orthdion_muon_set_dtypes(h, xt, gt)
+    od.orthdion_muon_set_scale(h, _scale(m, n))
+    od.orthdion_muon_set_schedule(h, [POLY[poly]] * steps, EPS)
+    return h
+
+
 def _plan(s, xt, gt):
     """Handles, workspace and pointer tables, made once as the program starts."""
     from paper_2605_16341_b200 import binding as od
     case = s["case"]
     if case["kind"] == "adamw":
-        plans = s["plans"] = _Plans(od.orthdion_adamw_destroy)
-
-        def make(k):
-            h = od.orthdion_adamw_create(k, BETA1, BETA2, ADAM_EPS, ADAM_ETA, ADAM_WD)
-            od.orthdion_adamw_set_dtypes(h, xt, gt)
-            return h
-        hs = [plans.get(k, lambda k=k: make(k)) for k in _lengths(case)]
+        hs = [_adamw_plan(k, xt, gt) for k in _lengths(case)]
         s["table"] = od.AdamWTable(hs, s["X"], s["M"], s["V"], s["G"])
         return
-    plans = s["plans"] = _Plans(od.orthdion_muon_destroy)
-
-    def make(m, n):
-        h = od.orthdion_muon_create(m, n, MU, ETA, WD, case.get("nesterov", True))
-        od.orthdion_muon_set_dtypes(h, xt, gt)
-        od.orthdion_muon_set_scale(h, _scale(m, n))
-        od.orthdion_muon_set_schedule(h, [POLY[case["poly"]]] * case["steps"], EPS)
-        return h
-    hs = [plans.get(mn, lambda mn=mn: make(*mn)) for mn in _shapes(case)]
+    hs = [_muon_plan(m, n, xt, gt, case.get("nesterov", True), case["poly"], case["steps"]) for m, n in _shapes(case)]
     s["ws"] = od.alloc_workspace(od.orthdion_muon_workspace_bytes_grouped(hs))
     if case["kind"] == "muon":
         s["table"] = od.MuonTable(hs, s["X"], s["M"], s["G"])
