@@ -73,6 +73,7 @@ typedef struct orthdion_plan* orthdion_t;
 #define ORTHDION_ERR_WORKSPACE     -4   /* workspace too small or misaligned                    */
 #define ORTHDION_ERR_CUDA          -5   /* a CUDA runtime call failed (launch, attribute, ...)  */
 #define ORTHDION_ERR_ALIGNMENT     -6   /* a matrix pointer is not 16-byte aligned              */
+#define ORTHDION_ERR_MEMORY        -7   /* host memory ran out (Muon and AdamW calls)           */
 
 /* per-matrix device status flags (bit mask) */
 #define ORTHDION_STATUS_SHIFTED_LEFT    1   /* left QR took three passes (shifted first pass,   */
@@ -255,6 +256,81 @@ int orthdion_rank_policy(double e_t, int32_t r_t, double ema_prev, int32_t r_min
  * a plan created with r_new (plans of different rank are packed separately by the grouped step). */
 int orthdion_resize_factor(const float* Q_old, int64_t n, int32_t r_old, float* Q_new, int32_t r_new,
                            const float* pad, void* stream);
+
+/* ---- full-rank steps: Newton-Schulz orthogonalisation and the Muon step --------------------------
+ * The full-rank counterpart of the low-rank step above, for matrices whose whole buffer is to be
+ * orthogonalised:
+ *
+ *   orthogonalise   X = B / (||B||_F + eps);  for each (a, b, c) of the schedule:
+ *                   A = X X^T (X^T X for m > n, the same polynomial),  X <- a X + (b A + c A^2) X
+ *   Muon step       M <- mu M + (1 - mu) G;   B = mu M + (1 - mu) G (nesterov) or B = M;
+ *                   X <- (1 - eta*wd) X - eta*scale * orthogonalise(B)
+ *
+ * Every step of the schedule maps a singular value s of X to s (a + b s^2 + c s^4).  Default: five steps of
+ * (3.4445, -4.7750, 2.0315), which leaves singular values from 0.7 to 1.2, and eps = 1e-7.
+ *
+ *  - The conventions above hold: device pointers, 16-byte aligned, row-major, M float32, X and G float32 or
+ *    bfloat16; work on `stream`, current device, caller's workspace (256-byte aligned), no device allocation,
+ *    no synchronisation; capture into a CUDA graph after one call outside of it.  Rows may lie further
+ *    apart than n entries (orthdion_muon_set_ld); what lies between them is not touched.
+ *  - Products run on the tensor cores in fp16 with fp32 sums.  passes = 1: one product of 11-bit operands, an error of
+ *    1e-3 to 4e-3 of the result; 3: two-term operands of 22 bits, three products, about 2e-6.  Default: 1 where X is
+ *    bfloat16 (its rounding is 1.7e-3), 3 where X is float32.  The norm is summed in 64 bits.
+ *  - A matrix of zeros has the result zero.  Where ||B||_F is below 1e-4 * eps the result, which is then small too, loses bits.
+ *  - A matrix whose B holds Inf or NaN (or a sum of squares beyond them) gets ORTHDION_STATUS_NONFINITE and keeps X and M (O).
+ *  - No matrix may stand twice in a call (ORTHDION_ERR_INVALID_ARG).  Matrices of equal plans share launches;
+ *    results per matrix do not depend on what else is in the call or on what the workspace held. */
+typedef struct orthdion_muon_plan* orthdion_muon_t;
+
+/* Plan for m x n matrices, min(m, n) <= 32768, 0 <= mu < 1.  Defaults: X and G bfloat16, scale 1. */
+int orthdion_muon_create(orthdion_muon_t* out, int64_t m, int64_t n, double mu, float eta, float wd, int32_t nesterov);
+int orthdion_muon_destroy(orthdion_muon_t h);
+int orthdion_muon_set_dtypes(orthdion_muon_t h, int32_t x_dtype, int32_t g_dtype);
+int orthdion_muon_set_lr(orthdion_muon_t h, float eta);
+int orthdion_muon_set_scale(orthdion_muon_t h, float scale);
+/* Entries from one row to the next, n <= ld <= 2^31 (X also: the result of an orthogonalisation). */
+int orthdion_muon_set_ld(orthdion_muon_t h, int64_t ld_x, int64_t ld_m, int64_t ld_g);
+/* steps (1 to 32) triples a, b, c.  Refused where it lets a singular value from [0, 1] grow beyond 8 or a
+ * factor |a| + |b| s^2 + |c| s^4 beyond 128: intermediate results are held in fp16. */
+int orthdion_muon_set_schedule(orthdion_muon_t h, int32_t steps, const float* abc, double eps);
+int orthdion_muon_set_passes(orthdion_muon_t h, int32_t passes);     /* 1 or 3; <= 0: the default rule */
+
+size_t orthdion_muon_workspace_bytes(orthdion_muon_t h);
+size_t orthdion_muon_workspace_bytes_grouped(const orthdion_muon_t* hs, int32_t count);
+
+/* O = orthogonalise(G), O of the plan's x_dtype and ld_x, G of its g_dtype and ld_g; O may be G where both are alike.
+ * mu, eta, wd, scale play no part. */
+int orthdion_orthogonalize(orthdion_muon_t h, const void* G, void* O, void* workspace, size_t workspace_bytes, void* stream);
+int orthdion_orthogonalize_grouped(const orthdion_muon_t* hs, int32_t count, const void* const* G, void* const* O,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* One Muon step; X and M are updated in place.  Grouped: host arrays of `count` device pointers. */
+int orthdion_muon_step(orthdion_muon_t h, void* X, float* M, const void* G, void* workspace, size_t workspace_bytes, void* stream);
+int orthdion_muon_step_grouped(const orthdion_muon_t* hs, int32_t count, void* const* X, float* const* M, const void* const* G,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/* The `count` status words (0, ORTHDION_STATUS_NONFINITE, ORTHDION_STATUS_WAIT_LIMIT) that the last of these calls left in
+ * the workspace, to host `flags` (synchronises `stream`). */
+int orthdion_muon_last_status(int32_t count, const void* workspace, void* stream, int32_t* flags);
+
+/* ---- AdamW step of the tensors that are no matrices of the steps above ------------------------------
+ * (embeddings, output heads, norm weights, biases: the paper's set-up steps those with AdamW)
+ *     m <- beta1 m + (1 - beta1) g;   v <- beta2 v + (1 - beta2) g^2;   t = steps taken, with this one
+ *     X <- X - eta (wd X + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps))
+ * Tensors are contiguous, of any length, 16-byte aligned; X and G float32 or bfloat16, m and v float32 (zeros before the first
+ * step); X, m, v in place.  step: DEVICE pointer to two int64, [0] the steps taken so far, which the call raises by one when it
+ * has read it (so a captured and replayed call goes on counting), [1] zero, the library's.  All tensors of a call are at the
+ * same step; a tensor may stand in it once.  No workspace. */
+typedef struct orthdion_adamw_plan* orthdion_adamw_t;
+
+/* 1 <= numel <= 2^40, 0 <= beta < 1, eps >= 0.  Defaults: X and G bfloat16. */
+int orthdion_adamw_create(orthdion_adamw_t* out, int64_t numel, double beta1, double beta2, float eps, float eta, float wd);
+int orthdion_adamw_destroy(orthdion_adamw_t h);
+int orthdion_adamw_set_dtypes(orthdion_adamw_t h, int32_t x_dtype, int32_t g_dtype);
+int orthdion_adamw_set_lr(orthdion_adamw_t h, float eta);
+int orthdion_adamw_step(orthdion_adamw_t h, void* X, float* M, float* V, const void* G, int64_t* step, void* stream);
+int orthdion_adamw_step_grouped(const orthdion_adamw_t* hs, int32_t count, void* const* X, float* const* M, float* const* V,
+                                const void* const* G, int64_t* step, void* stream);
 
 /* Number of kernels this library has launched so far in this process (monotonic). */
 int64_t orthdion_launch_count(void);

@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import os
 import subprocess
+import tempfile
 
 import torch
 
@@ -24,10 +25,11 @@ ENGINE_TENSOR, ENGINE_SIMT = 0, 1
 STATUS_SHIFTED_LEFT, STATUS_SHIFTED_RIGHT, STATUS_RANK_DEFICIENT = 1, 2, 4
 STATUS_NONFINITE, STATUS_ZERO_COLUMN, STATUS_WAIT_LIMIT = 8, 16, 32
 
-ERRORS = {0: "OK", -1: "INVALID_ARG", -2: "RANK", -3: "NULL", -4: "WORKSPACE", -5: "CUDA", -6: "ALIGNMENT"}
+ERRORS = {0: "OK", -1: "INVALID_ARG", -2: "RANK", -3: "NULL", -4: "WORKSPACE", -5: "CUDA", -6: "ALIGNMENT", -7: "MEMORY"}
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "--shared", "-Xcompiler", "-fPIC"]
+              "-Xcompiler", "-fPIC"]
+SOURCES = ["orthdion.cu", "muon.cu"]      # the low-rank steps; the full-rank steps and AdamW
 
 
 class OrthDionError(RuntimeError):
@@ -37,13 +39,15 @@ class OrthDionError(RuntimeError):
 
 
 def build_library(verbose: bool = False) -> str:
-    """Compile csrc/orthdion.cu for sm_100a into liborthdion.so next to this file."""
-    src = os.path.join(CSRC, "orthdion.cu")
-    cmd = ["nvcc", *NVCC_FLAGS, "-o", LIB_PATH, src]
-    if verbose:
-        cmd.insert(1, "-Xptxas")
-        cmd.insert(2, "-v")
-    subprocess.run(cmd, check=True)
+    """Compile csrc/*.cu for sm_100a, side by side, into liborthdion.so next to this file."""
+    extra = ["-Xptxas", "-v"] if verbose else []
+    with tempfile.TemporaryDirectory() as tmp:
+        objs = [os.path.join(tmp, src + ".o") for src in SOURCES]
+        jobs = [subprocess.Popen(["nvcc", *extra, *NVCC_FLAGS, "-c", "-o", obj, os.path.join(CSRC, src)])
+                for src, obj in zip(SOURCES, objs)]
+        for job in [j for j in jobs if j.wait() != 0]:
+            raise subprocess.CalledProcessError(job.returncode, job.args)
+        subprocess.run(["nvcc", *NVCC_FLAGS, "--shared", "-o", LIB_PATH, *objs], check=True)
     return LIB_PATH
 
 
@@ -95,9 +99,37 @@ def lib() -> ctypes.CDLL:
     L.orthdion_stage_count.restype = i32
     L.orthdion_stage_name.argtypes = [i32]
     L.orthdion_stage_name.restype = ctypes.c_char_p
+    f64 = ctypes.c_double
+    L.orthdion_muon_create.argtypes = [pvp, i64, i64, f64, f32, f32, i32]
+    L.orthdion_muon_destroy.argtypes = [vp]
+    L.orthdion_muon_set_dtypes.argtypes = [vp, i32, i32]
+    L.orthdion_muon_set_lr.argtypes = [vp, f32]
+    L.orthdion_muon_set_scale.argtypes = [vp, f32]
+    L.orthdion_muon_set_ld.argtypes = [vp, i64, i64, i64]
+    L.orthdion_muon_set_schedule.argtypes = [vp, i32, ctypes.POINTER(f32), f64]
+    L.orthdion_muon_set_passes.argtypes = [vp, i32]
+    L.orthdion_muon_workspace_bytes.argtypes = [vp]
+    L.orthdion_muon_workspace_bytes.restype = sz
+    L.orthdion_muon_workspace_bytes_grouped.argtypes = [pvp, i32]
+    L.orthdion_muon_workspace_bytes_grouped.restype = sz
+    L.orthdion_orthogonalize.argtypes = [vp, vp, vp, vp, sz, vp]
+    L.orthdion_orthogonalize_grouped.argtypes = [pvp, i32, pvp, pvp, vp, sz, vp]
+    L.orthdion_muon_step.argtypes = [vp, vp, vp, vp, vp, sz, vp]
+    L.orthdion_muon_step_grouped.argtypes = [pvp, i32, pvp, pvp, pvp, vp, sz, vp]
+    L.orthdion_muon_last_status.argtypes = [i32, vp, vp, ctypes.POINTER(i32)]
+    L.orthdion_adamw_create.argtypes = [pvp, i64, f64, f64, f32, f32, f32]
+    L.orthdion_adamw_destroy.argtypes = [vp]
+    L.orthdion_adamw_set_dtypes.argtypes = [vp, i32, i32]
+    L.orthdion_adamw_set_lr.argtypes = [vp, f32]
+    L.orthdion_adamw_step.argtypes = [vp, vp, vp, vp, vp, vp, vp]
+    L.orthdion_adamw_step_grouped.argtypes = [pvp, i32, pvp, pvp, pvp, pvp, vp, vp]
     for name in ("create", "destroy", "set_dtypes", "set_lr", "set_scale", "set_ef", "set_engine",
                  "set_passes", "step", "step_grouped", "step_noalloc", "get_factors", "last_status",
-                 "set_diagnostics", "last_diagnostics", "rank_policy", "resize_factor", "set_concurrency", "shard_phase", "shard_reduce_buffer"):
+                 "set_diagnostics", "last_diagnostics", "rank_policy", "resize_factor", "set_concurrency", "shard_phase", "shard_reduce_buffer",
+                 "muon_create", "muon_destroy", "muon_set_dtypes", "muon_set_lr", "muon_set_scale", "muon_set_ld",
+                 "muon_set_schedule", "muon_set_passes", "orthogonalize", "orthogonalize_grouped", "muon_step",
+                 "muon_step_grouped", "muon_last_status", "adamw_create", "adamw_destroy", "adamw_set_dtypes", "adamw_set_lr",
+                 "adamw_step", "adamw_step_grouped"):
         getattr(L, "orthdion_" + name).restype = i32
     _lib = L
     return L
@@ -110,7 +142,13 @@ EXPORTED = ["orthdion_create", "orthdion_destroy", "orthdion_set_dtypes", "orthd
             "orthdion_set_concurrency", "orthdion_shard_phase", "orthdion_shard_reduce_buffer", "orthdion_set_diagnostics", "orthdion_last_diagnostics", "orthdion_rank_policy",
             "orthdion_resize_factor", "orthdion_version",
             "orthdion_launch_count", "orthdion_profile_begin", "orthdion_profile_end", "orthdion_stage_count",
-            "orthdion_stage_name"]
+            "orthdion_stage_name",
+            "orthdion_muon_create", "orthdion_muon_destroy", "orthdion_muon_set_dtypes", "orthdion_muon_set_lr", "orthdion_muon_set_scale",
+            "orthdion_muon_set_ld", "orthdion_muon_set_schedule", "orthdion_muon_set_passes", "orthdion_muon_workspace_bytes",
+            "orthdion_muon_workspace_bytes_grouped", "orthdion_orthogonalize", "orthdion_orthogonalize_grouped",
+            "orthdion_muon_step", "orthdion_muon_step_grouped", "orthdion_muon_last_status",
+            "orthdion_adamw_create", "orthdion_adamw_destroy", "orthdion_adamw_set_dtypes", "orthdion_adamw_set_lr",
+            "orthdion_adamw_step", "orthdion_adamw_step_grouped"]
 
 
 def _check(code, where):
@@ -306,6 +344,209 @@ def orthdion_resize_factor(Q_old, Q_new, pad=None, stream=None):
     _check(lib().orthdion_resize_factor(_dev_ptr(Q_old, "Q_old"), n, r_old, _dev_ptr(Q_new, "Q_new"), r_new,
                                         _dev_ptr(pad, "pad") if pad is not None else None,
                                         _stream_ptr(stream)), "orthdion_resize_factor")
+
+
+# ---- full-rank steps (Newton-Schulz orthogonalisation, Muon) and AdamW ------------------------------
+def orthdion_muon_create(m, n, mu, eta, wd, nesterov=True) -> int:
+    h = ctypes.c_void_p()
+    _check(lib().orthdion_muon_create(ctypes.byref(h), m, n, mu, eta, wd, int(nesterov)), "orthdion_muon_create")
+    _plans[h.value] = _Plan(m, n, [n, n, n], [torch.bfloat16, torch.bfloat16])
+    return h.value
+
+
+def orthdion_muon_destroy(h):
+    _check(lib().orthdion_muon_destroy(h), "orthdion_muon_destroy")
+    _plans.pop(h, None)
+
+
+def orthdion_muon_set_dtypes(h, x_dtype, g_dtype):
+    _check(lib().orthdion_muon_set_dtypes(h, _dt(x_dtype), _dt(g_dtype)), "orthdion_muon_set_dtypes")
+    _plans[h].dtypes = [x_dtype, g_dtype]
+
+
+def orthdion_muon_set_lr(h, eta):
+    _check(lib().orthdion_muon_set_lr(h, eta), "orthdion_muon_set_lr")
+
+
+def orthdion_muon_set_scale(h, scale):
+    _check(lib().orthdion_muon_set_scale(h, scale), "orthdion_muon_set_scale")
+
+
+def orthdion_muon_set_ld(h, ld_x, ld_m, ld_g):
+    """Entries from one row to the next of X (or the result), M and G, for matrices that are columns of wider ones."""
+    _check(lib().orthdion_muon_set_ld(h, ld_x, ld_m, ld_g), "orthdion_muon_set_ld")
+    _plans[h].ld = [ld_x, ld_m, ld_g]
+
+
+def orthdion_muon_set_schedule(h, coefficients, eps=1e-7):
+    """coefficients: one triple (a, b, c) per step of X <- a X + (b A + c A^2) X."""
+    flat = [float(v) for abc in coefficients for v in abc]
+    if len(flat) != 3 * len(coefficients):
+        raise ValueError("coefficients: a list of triples (a, b, c)")
+    _check(lib().orthdion_muon_set_schedule(h, len(coefficients), (ctypes.c_float * max(1, len(flat)))(*flat), eps),
+           "orthdion_muon_set_schedule")
+
+
+def orthdion_muon_set_passes(h, passes):
+    _check(lib().orthdion_muon_set_passes(h, passes), "orthdion_muon_set_passes")
+
+
+def orthdion_muon_workspace_bytes(h) -> int:
+    return lib().orthdion_muon_workspace_bytes(h)
+
+
+def orthdion_muon_workspace_bytes_grouped(hs) -> int:
+    return lib().orthdion_muon_workspace_bytes_grouped(_harr(hs), len(hs))
+
+
+class _Plan:
+    """What the binding checks a tensor against before its pointer is handed on."""
+
+    def __init__(self, m, n, ld, dtypes):
+        self.m, self.n, self.ld, self.dtypes = m, n, ld, dtypes
+
+
+_plans: dict = {}
+
+
+def _matrix_ptr(t, name, h, ld, dtype, device):
+    p = _plans.get(h)
+    if p is None:
+        raise OrthDionError(-1, f"{name}: no such plan")
+    if not t.is_cuda or t.device != device:
+        raise ValueError(f"{name} must be a CUDA tensor on the current device")
+    if tuple(t.shape) != (p.m, p.n) or t.dtype != dtype:
+        raise ValueError(f"{name}: the plan has {p.m} x {p.n} {dtype}, got {tuple(t.shape)} {t.dtype}")
+    if (p.n > 1 and t.stride(1) != 1) or (p.m > 1 and t.stride(0) != ld):
+        raise ValueError(f"{name}: rows must be contiguous and {ld} entries apart (orthdion_muon_set_ld)")
+    return t.data_ptr()
+
+
+def _muon_ptrs(h, X, M, G):
+    """Pointers of one matrix's tensors (M None: an orthogonalisation)."""
+    p, dev = _plans.get(h), torch.device("cuda", torch.cuda.current_device())
+    if p is None:
+        raise OrthDionError(-1, "no such plan")
+    return (_matrix_ptr(X, "X", h, p.ld[0], p.dtypes[0], dev),
+            None if M is None else _matrix_ptr(M, "M", h, p.ld[1], torch.float32, dev),
+            _matrix_ptr(G, "G", h, p.ld[2], p.dtypes[1], dev))
+
+
+def orthdion_orthogonalize(h, G, O, workspace, stream=None):
+    """O = the Newton-Schulz orthogonalisation of G.  O has the plan's x_dtype, G its g_dtype."""
+    o, _, g = _muon_ptrs(h, O, None, G)
+    _check(lib().orthdion_orthogonalize(h, g, o, _dev_ptr(workspace, "workspace"),
+                                        workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
+           "orthdion_orthogonalize")
+
+
+def orthdion_muon_step(h, X, M, G, workspace, stream=None):
+    """One Muon step of one matrix; X and M are updated in place."""
+    x, m, g = _muon_ptrs(h, X, M, G)
+    _check(lib().orthdion_muon_step(h, x, m, g, _dev_ptr(workspace, "workspace"),
+                                    workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
+           "orthdion_muon_step")
+
+
+class MuonTable:
+    """Host arrays of device pointers for the grouped full-rank calls, built once and reused.  Ms None: a table for
+    orthdion_orthogonalize_grouped, Xs the results."""
+
+    def __init__(self, hs, Xs, Ms, Gs):
+        n = len(hs)
+        if not (n and len(Xs) == len(Gs) == n and (Ms is None or len(Ms) == n)):
+            raise ValueError("one plan, X, M and G per matrix")
+        ptrs = [_muon_ptrs(h, Xs[i], None if Ms is None else Ms[i], Gs[i]) for i, h in enumerate(hs)]
+        arr = ctypes.c_void_p * n
+        self.n, self.hs = n, arr(*hs)
+        self.X, self.G = arr(*[p[0] for p in ptrs]), arr(*[p[2] for p in ptrs])
+        self.M = None if Ms is None else arr(*[p[1] for p in ptrs])
+        self._keep = (list(Xs), None if Ms is None else list(Ms), list(Gs))
+
+
+def orthdion_orthogonalize_grouped(table: MuonTable, workspace, stream=None):
+    _check(lib().orthdion_orthogonalize_grouped(table.hs, table.n, table.G, table.X, _dev_ptr(workspace, "workspace"),
+                                                workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
+           "orthdion_orthogonalize_grouped")
+
+
+def orthdion_muon_step_grouped(table: MuonTable, workspace, stream=None):
+    _check(lib().orthdion_muon_step_grouped(table.hs, table.n, table.X, table.M, table.G, _dev_ptr(workspace, "workspace"),
+                                            workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
+           "orthdion_muon_step_grouped")
+
+
+def orthdion_muon_last_status(count, workspace, stream=None):
+    flags = (ctypes.c_int32 * count)()
+    _check(lib().orthdion_muon_last_status(count, _dev_ptr(workspace, "workspace"), _stream_ptr(stream), flags),
+           "orthdion_muon_last_status")
+    return list(flags)
+
+
+def orthdion_adamw_create(numel, beta1, beta2, eps, eta, wd) -> int:
+    h = ctypes.c_void_p()
+    _check(lib().orthdion_adamw_create(ctypes.byref(h), numel, beta1, beta2, eps, eta, wd), "orthdion_adamw_create")
+    _plans[h.value] = _Plan(numel, 1, None, [torch.bfloat16, torch.bfloat16])
+    return h.value
+
+
+def orthdion_adamw_destroy(h):
+    _check(lib().orthdion_adamw_destroy(h), "orthdion_adamw_destroy")
+    _plans.pop(h, None)
+
+
+def orthdion_adamw_set_dtypes(h, x_dtype, g_dtype):
+    _check(lib().orthdion_adamw_set_dtypes(h, _dt(x_dtype), _dt(g_dtype)), "orthdion_adamw_set_dtypes")
+    _plans[h].dtypes = [x_dtype, g_dtype]
+
+
+def orthdion_adamw_set_lr(h, eta):
+    _check(lib().orthdion_adamw_set_lr(h, eta), "orthdion_adamw_set_lr")
+
+
+class AdamWTable:
+    """Host arrays of device pointers for orthdion_adamw_step_grouped, built once and reused."""
+
+    def __init__(self, hs, Xs, Ms, Vs, Gs):
+        n = len(hs)
+        if not (n and len(Xs) == len(Ms) == len(Vs) == len(Gs) == n):
+            raise ValueError("one plan, X, M, V and G per tensor")
+        dev = torch.device("cuda", torch.cuda.current_device())
+
+        def ptr(t, name, h, dtype):
+            p = _plans.get(h)
+            if p is None:
+                raise OrthDionError(-1, f"{name}: no such plan")
+            if not t.is_cuda or t.device != dev:
+                raise ValueError(f"{name} must be a CUDA tensor on the current device")
+            if t.numel() != p.m or t.dtype != dtype:
+                raise ValueError(f"{name}: the plan has {p.m} entries of {dtype}, got {t.numel()} of {t.dtype}")
+            return _dev_ptr(t, name)
+
+        arr = ctypes.c_void_p * n
+        xt, gt = [[_plans[h].dtypes[k] if h in _plans else None for h in hs] for k in (0, 1)]
+        self.n, self.hs = n, arr(*hs)
+        self.X = arr(*[ptr(t, "X", h, d) for t, h, d in zip(Xs, hs, xt)])
+        self.M = arr(*[ptr(t, "M", h, torch.float32) for t, h in zip(Ms, hs)])
+        self.V = arr(*[ptr(t, "V", h, torch.float32) for t, h in zip(Vs, hs)])
+        self.G = arr(*[ptr(t, "G", h, d) for t, h, d in zip(Gs, hs, gt)])
+        self._keep = (list(Xs), list(Ms), list(Vs), list(Gs))
+
+
+def _step_ptr(step) -> int:
+    if step.dtype != torch.int64 or step.numel() != 2:
+        raise ValueError("step: two int64, the steps taken and a zero")
+    return _dev_ptr(step, "step")
+
+
+def orthdion_adamw_step_grouped(table: AdamWTable, step, stream=None):
+    """One AdamW step of every tensor of the table; step: CUDA tensor of two int64, [steps taken, 0]."""
+    _check(lib().orthdion_adamw_step_grouped(table.hs, table.n, table.X, table.M, table.V, table.G, _step_ptr(step),
+                                             _stream_ptr(stream)), "orthdion_adamw_step_grouped")
+
+
+def orthdion_adamw_step(h, X, M, V, G, step, stream=None):
+    orthdion_adamw_step_grouped(AdamWTable([h], [X], [M], [V], [G]), step, stream)
 
 
 def orthdion_launch_count() -> int:

@@ -23,6 +23,7 @@
 #include <cstdio>
 
 #include "common.cuh"
+#include "tcgen05.cuh"
 #include "factor_tc.cuh"
 #include "launch.cuh"
 #include "qr_small.cuh"
@@ -31,7 +32,6 @@
 namespace od {
 namespace tc {
 
-constexpr int BM = 128;                      // tile rows (MMA M)
 constexpr int BK = 64;                       // depth of one A tile: 64 bf16 = one 128-byte row
 constexpr int A_TERM_BYTES = 128 * 128;      // one 128 x 64 bf16 tile
 constexpr int A_RING_BYTES = 4 * A_TERM_BYTES;   // two slots of two terms, or four slots of one
@@ -42,7 +42,6 @@ constexpr int STORE_STAGING_BYTES = 4096;    // epilogue staging of the products
 // ... of the fused pass: 32 x 32 slabs of M, G and X per warp (xg bit 0: G is bf16, bit 1: X is)
 __host__ __device__ constexpr int slab_bytes(int xg) { return 4096 + ((xg & 1) ? 2048 : 4096) + ((xg & 2) ? 2048 : 4096); }
 constexpr int SMEM_LIMIT = 227 * 1024;
-constexpr long long WAIT_LIMIT_CYCLES = 4000000000LL;   // about two seconds
 
 enum AMode : int { A_IMG_K = 0, A_IMG_MN = 1, A_BUF_ROW = 2, A_BUF_COL = 3 };
 enum NMode : int { N_IMG_K = 0, N_IMG_MN = 1 };
@@ -109,212 +108,6 @@ struct GemmArgs {
     alignas(64) CUtensorMap map_n1;
     alignas(64) CUtensorMap map_n2;
 };
-
-// ------------------------------------------------------------------------------------------
-// PTX wrappers
-// ------------------------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t smem_u32(const void* p) {
-    return static_cast<uint32_t>(__cvta_generic_to_shared(p));
-}
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive_expect_tx(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
-}
-// Bounded wait: gives up after WAIT_LIMIT_CYCLES or as soon as another role of the CTA gave up.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-    if (mbar_try_wait(bar, parity)) return true;
-    const long long t0 = clock64();
-    int spins = 0;
-    while (!mbar_try_wait(bar, parity)) {
-        if ((++spins & 63) == 0) {
-            if (*abort_flag) return false;
-            if (clock64() - t0 > WAIT_LIMIT_CYCLES) { *abort_flag = 1; return false; }
-        }
-    }
-    return true;
-}
-// One tiled TMA load: the box of `map` at (0, row, panel, plane, matrix) -> shared memory, laid
-// out [term][panel][row][128 bytes]; completes on the mbarrier with the full box size.
-__device__ __forceinline__ void tma_load_box(uint32_t dst, const CUtensorMap* map, int row, int panel, int plane,
-                                             int matrix, uint32_t bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
-        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(panel), "r"(plane), "r"(matrix), "r"(bar)
-        : "memory");
-}
-// ---- CTA pairs (clusters of two CTAs on neighbouring SMs, tcgen05 cta_group::2) ----------------
-// One MMA instruction of the pair's leader (cluster rank 0) multiplies M = 256 rows: each CTA
-// supplies its own 128 rows of A and HALF of the N-side operand, and receives its 128 rows of the
-// result in its own tensor memory.  Per CTA that halves the N-side bytes that are fetched from L2
-// and read from shared memory by the tensor core.  Barriers that gather both CTAs (operand
-// "full", accumulator "empty") live in the leader and are reached by remote arrives; barriers
-// that release (operand "empty", accumulator "full") live in each CTA and are reached by the
-// leader's multicast commit.  All of them keep the default (CTA-scope) semantics of the single-CTA
-// barriers: with release/acquire at cluster scope on every arrive and wait the same kernels ran up
-// to twice as long (the producer thread then pays a cluster-wide fence per load).
-__device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr) {
-    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive_expect_tx_remote(uint32_t cluster_addr, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;"
-                 ::"r"(cluster_addr), "r"(bytes) : "memory");
-}
-// Tiled TMA load of a CTA of a pair: the data lands in this CTA's shared memory, the bytes are
-// counted on the mbarrier at cluster address `bar` (the leader's).
-__device__ __forceinline__ void tma_load_box_pair(uint32_t dst, const CUtensorMap* map, int row, int panel, int plane,
-                                                  int matrix, uint32_t bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
-        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(panel), "r"(plane), "r"(matrix), "r"(bar)
-        : "memory");
-}
-__device__ __forceinline__ void tmem_alloc_pair(uint32_t slot_smem, uint32_t ncols) {
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot_smem), "r"(ncols) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr, uint32_t ncols) {
-    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
-}
-// D[tmem of both CTAs] (+)= A * B^T with M = 256; issued by one thread of the leader.
-__device__ __forceinline__ void umma_bf16_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
-                                               uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
-}
-// the mbarrier at offset `bar` of BOTH CTAs arrives once every MMA issued so far has completed
-__device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
-    asm volatile(
-        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-        ::"r"(bar), "h"((uint16_t)3) : "memory");
-}
-
-__device__ __forceinline__ void prefetch_tensor_map(const CUtensorMap* map) {
-    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
-}
-// Asynchronous 16-byte copy global -> shared (no register staging), grouped per thread.
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ void fence_async_smem() {
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-}
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-
-__device__ __forceinline__ void tmem_alloc(uint32_t slot_smem, uint32_t ncols) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot_smem), "r"(ncols) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void tmem_dealloc(uint32_t taddr, uint32_t ncols) {
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
-}
-// D[tmem] (+)= A[smem] * B[smem]^T, bf16 inputs, fp32 accumulation; issued by one thread.
-__device__ __forceinline__ void umma_bf16(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
-                                          uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
-}
-// mbarrier arrives once every MMA issued so far by this thread has completed
-__device__ __forceinline__ void umma_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
-          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
-        : "r"(taddr) : "memory");
-}
-__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-
-// Shared-memory matrix descriptor, 128-byte swizzle.  K-major: rows of 128 bytes, 8-row groups
-// 1024 bytes apart (stride offset), leading offset unused.  MN-major: lbo = distance between
-// 64-element groups along M/N, sbo = distance between 8-deep groups along K.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
-    uint64_t d = 0;
-    d |= (uint64_t)((addr & 0x3FFFFu) >> 4);
-    d |= (uint64_t)((lbo_bytes >> 4) & 0x3FFFu) << 16;
-    d |= (uint64_t)((sbo_bytes >> 4) & 0x3FFFu) << 32;
-    d |= (uint64_t)1 << 46;     // descriptor version of this architecture
-    d |= (uint64_t)2 << 61;     // 128-byte swizzle
-    return d;
-}
-// Instruction descriptor: fp32 accumulate, bf16 A and B, M = 128, N = n; a_mn / b_mn = 1 for an
-// MN-major A / B operand (0: K-major).
-// fmt: operand format, 1 = bf16, 0 = fp16 (both operands alike).
-// m: rows of the instruction, 128, or 256 for an instruction of a CTA pair.
-__device__ __forceinline__ uint32_t instr_desc(uint32_t n, uint32_t a_mn, uint32_t b_mn, uint32_t fmt = 1u,
-                                               uint32_t m = (uint32_t)BM) {
-    return (1u << 4) | (fmt << 7) | (fmt << 10) | (a_mn << 15) | (b_mn << 16) | ((n >> 3) << 17) |
-           ((m >> 4) << 24);
-}
-template <bool PAIR>
-__device__ __forceinline__ void umma_any(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
-                                         uint32_t accumulate) {
-    if (PAIR) umma_bf16_pair(d_tmem, adesc, bdesc, idesc, accumulate);
-    else umma_bf16(d_tmem, adesc, bdesc, idesc, accumulate);
-}
-// The same with the descriptors given as halves (the high one is constant), always adding to D.
-template <bool PAIR>
-__device__ __forceinline__ void umma_add(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi,
-                                         uint32_t idesc) {
-    if (PAIR)
-        asm volatile("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%1, %2};\n\tmov.b64 b, {%3, %4};\n\t"
-                     "tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %5, 1;\n\t}"
-                     ::"r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc) : "memory");
-    else
-        asm volatile("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%1, %2};\n\tmov.b64 b, {%3, %4};\n\t"
-                     "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, 1;\n\t}"
-                     ::"r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc) : "memory");
-}
-template <bool PAIR>
-__device__ __forceinline__ void umma_halves(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi,
-                                            uint32_t idesc, uint32_t accumulate) {
-    umma_any<PAIR>(d_tmem, ((uint64_t)a_hi << 32) | a_lo, ((uint64_t)b_hi << 32) | b_lo, idesc, accumulate);
-}
-// NS 16-deep slices in one straight line: descriptors by additions, nothing else between the instructions.
-template <bool PAIR, int NS, bool THREE>
-__device__ __forceinline__ void umma_slices(uint32_t d, uint32_t a, uint32_t a_hi, uint32_t b, uint32_t b_hi, uint32_t a_step,
-                                            uint32_t b_step, uint32_t a_term, uint32_t b_term, uint32_t idesc, uint32_t accum) {
-#pragma unroll
-    for (int j = 0; j < NS; ++j) {
-        const uint32_t aj = a + j * a_step, bj = b + j * b_step;
-        if (j == 0) umma_halves<PAIR>(d, aj, a_hi, bj, b_hi, idesc, accum);
-        else umma_add<PAIR>(d, aj, a_hi, bj, b_hi, idesc);
-        if (THREE) {
-            umma_add<PAIR>(d, aj, a_hi, bj + b_term, b_hi, idesc);
-            umma_add<PAIR>(d, aj + a_term, a_hi, bj, b_hi, idesc);
-        }
-    }
-}
-template <bool PAIR>
-__device__ __forceinline__ void commit_any(uint32_t bar) {
-    if (PAIR) umma_commit_pair(bar);
-    else umma_commit(bar);
-}
 
 __device__ __forceinline__ void load8(const void* base, int64_t idx, int is_bf16, float (&v)[8]) {
     if (is_bf16) {
@@ -1512,23 +1305,6 @@ inline ImgRef img_view(const ImgRef& im, int64_t rows) {
     return v;
 }
 
-// cuTensorMapEncodeTiled, fetched through the runtime so that the library does not link libcuda.
-typedef CUresult (*TensorMapEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                      const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                      CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-inline TensorMapEncodeFn tensor_map_encoder() {
-    static TensorMapEncodeFn fn = nullptr;
-    static bool tried = false;
-    if (!tried) {
-        tried = true;
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            fn = reinterpret_cast<TensorMapEncodeFn>(p);
-    }
-    return fn;
-}
 // 5-d map over the images `img` of all matrices of a batch: (64 bf16, rows, panels, terms, matrix),
 // with the box (64, box_rows, box_panels, box_terms, 1).  The images are stored pre-swizzled, so
 // the copy itself does not swizzle; out-of-range parts of a box read as zeros.
@@ -1551,22 +1327,6 @@ inline void encode_img_map(CUtensorMap* map, const Batch& b, const ImgRef& img, 
         std::fprintf(stderr, "orthdion: cuTensorMapEncodeTiled failed (%d)\n", (int)r);
         engine_error() = 2;
     }
-}
-
-// Multiprocessor count of the current device (looked up once per device ordinal).
-constexpr int kMaxDevices = 64;
-inline int sm_count() {
-    static std::atomic<int> cached[kMaxDevices] = {};
-    int dev = 0;
-    cudaGetDevice(&dev);
-    if (dev < 0 || dev >= kMaxDevices) dev = 0;
-    int n = cached[dev].load(std::memory_order_relaxed);
-    if (n <= 0) {
-        cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
-        if (n <= 0) n = 148;
-        cached[dev].store(n, std::memory_order_relaxed);
-    }
-    return n;
 }
 
 // Which instantiations exist as CTA-pair kernels: every product with an MN-major N-side (the two
