@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "adamw.cuh"
+#include "lanes.cuh"
 #include "newton_schulz.cuh"
 
 using namespace od;
@@ -19,7 +20,8 @@ using namespace od;
 namespace {
 constexpr uint32_t kMuonMagic = 0x0D10B0E5u, kAdamWMagic = 0x0D10ADA3u;
 constexpr int32_t kMaxSteps = 32;
-constexpr size_t kScratchBudget = (size_t)2 << 30;     // per launch batch
+constexpr size_t kScratchBudget = (size_t)1 << 30;     // per launch batch
+constexpr int kPlannedLanes = 4;
 constexpr int kTwoTermChunk = 1;                        // depth blocks of 64 that two-plane products sum in tensor memory
 }  // namespace
 
@@ -114,11 +116,24 @@ Scratch scratch_layout(const orthdion_muon_plan* p, int count) {
     return c;
 }
 
-// Launch batches: matrices of one class, so many that the scratch stays within the budget.
-std::vector<std::vector<int>> make_batches(const orthdion_muon_t* hs, int32_t count, size_t* scratch) {
-    std::vector<std::vector<int>> out;
+// Launch batches of a call (matrices of one class, so many that the scratch stays within the budget), in the order in which they are
+// enqueued, and the lanes they run on: one chain of launches leaves multiprocessors idle at the end of each, which those of another lane fill.
+// Every lane has scratch of its own.
+struct Batching {
+    std::vector<std::vector<int>> batches;
+    std::vector<size_t> off;           // scratch offset
+    int lanes = 1;                     // batch i runs on lane i % lanes
+    size_t scratch = 0;
+};
+
+double cost(const orthdion_muon_plan* p, size_t count) {
+    const double s = (double)std::min(p->m, p->n), l = (double)std::max(p->m, p->n);
+    return (double)count * p->steps * s * s * (3 * l + s) * (p->passes == 3 ? 3 : 1);
+}
+
+Batching make_batches(const orthdion_muon_t* hs, int32_t count) {
+    Batching out;
     std::vector<char> done(count, 0);
-    *scratch = 0;
     for (int i = 0; i < count; ++i) {
         if (done[i]) continue;
         std::vector<int> cls;
@@ -127,11 +142,17 @@ std::vector<std::vector<int>> make_batches(const orthdion_muon_t* hs, int32_t co
         const size_t per = scratch_layout(hs[i], 1).bytes;
         const size_t cap = std::min<size_t>(std::max<size_t>(1, kScratchBudget / per), ns::MAX_BATCH);
         const size_t nb = (cls.size() + cap - 1) / cap, bs = (cls.size() + nb - 1) / nb;
-        for (size_t b = 0; b < cls.size(); b += bs) {
-            out.emplace_back(cls.begin() + b, cls.begin() + std::min(cls.size(), b + bs));
-            *scratch = std::max(*scratch, scratch_layout(hs[i], (int)out.back().size()).bytes);
-        }
+        for (size_t b = 0; b < cls.size(); b += bs) out.batches.emplace_back(cls.begin() + b, cls.begin() + std::min(cls.size(), b + bs));
     }
+    // heaviest first
+    std::stable_sort(out.batches.begin(), out.batches.end(),
+                     [&](const auto& a, const auto& b) { return cost(hs[a[0]], a.size()) > cost(hs[b[0]], b.size()); });
+    out.lanes = std::min<int>(kPlannedLanes, (int)out.batches.size());
+    std::vector<size_t> most(out.lanes, 0), at(out.lanes, 0);
+    for (size_t b = 0; b < out.batches.size(); ++b)
+        most[b % out.lanes] = std::max(most[b % out.lanes], scratch_layout(hs[out.batches[b][0]], (int)out.batches[b].size()).bytes);
+    for (int l = 0; l < out.lanes; ++l) { at[l] = out.scratch; out.scratch += most[l]; }
+    for (size_t b = 0; b < out.batches.size(); ++b) out.off.push_back(at[b % out.lanes]);
     return out;
 }
 
@@ -178,7 +199,6 @@ void launch_gemm(const Chain& c, ns::GemmArgs& g, const Image& a, const Image& b
     if (!encode(&g.map_a, a.base, a.cols, a.rows, TERMS, c.count, a.pitch, a.term, a.mat, g.a_mn ? 64 : 128, TERMS)) return;
     if (!encode(&g.map_b, b.base, b.cols, b.rows, TERMS, c.count, b.pitch, b.term, b.mat, g.b_mn ? 64 : NB, TERMS)) return;
     if (out) {
-        if (!encode(&g.map_out, out->base, out->cols, out->rows, TERMS, c.count, out->pitch, out->term, out->mat, 32, 1)) return;
         g.out = reinterpret_cast<__half*>(out->base);
         g.pitch = out->pitch; g.term_stride = out->term; g.mat_stride = out->mat;
     }
@@ -254,6 +274,8 @@ void apply_product(const Chain& c, const Image& pm, const Image& x, const Image*
         g.x_bf16 = c.p->x_dtype == ORTHDION_DTYPE_BF16;
         g.wc = 1.f - c.p->eta * c.p->wd; g.wd = c.p->eta * c.p->scale;
         g.ld_x = c.p->ld_x;
+        const int64_t whole = g.x_bf16 ? 8 : 4;
+        g.x_vec = c.p->n % whole == 0 && c.p->ld_x % whole == 0;
         product<ns::EPI_FINAL>(c, g, a, b, nullptr, *table);
     }
 }
@@ -360,23 +382,38 @@ int run_call(const orthdion_muon_t* hs, int32_t count, void* const* X, float* co
     }
     if (twice(X, count) || (update && twice(reinterpret_cast<const void* const*>(M), count))) return ORTHDION_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(workspace) % 256) return ORTHDION_ERR_WORKSPACE;
-    size_t scratch = 0;
-    const auto batches = make_batches(hs, count, &scratch);
-    if (workspace_bytes < status_bytes(count) + scratch) return ORTHDION_ERR_WORKSPACE;
+    const Batching bt = make_batches(hs, count);
+    if (workspace_bytes < status_bytes(count) + bt.scratch) return ORTHDION_ERR_WORKSPACE;
     int e = ensure_attributes();
     if (e) return e;
     char* ws = reinterpret_cast<char*>(workspace);
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const int lanes = std::min(bt.lanes, g_lanes.load());
+    DeviceLanes* dl = lanes > 1 ? device_lanes() : nullptr;
+    std::unique_lock<std::mutex> lock;
+    if (dl) {
+        lock = std::unique_lock<std::mutex>(dl->mu);
+        cudaEventRecord(dl->fork, st);
+        for (int l = 0; l < lanes; ++l) cudaStreamWaitEvent(dl->lane[l], dl->fork, 0);
+    }
     engine_error() = 0;
-    overlap_launches() = true;
-    for (const auto& idx : batches) {
+    overlap_launches() = dl == nullptr;      // (CTAs that wait for one chain's next launch would keep the others' off the multiprocessors)
+    for (size_t b = 0; b < bt.batches.size() && !engine_error(); ++b) {
+        const auto& idx = bt.batches[b];
         ns::Table t{};
         t.count = (int32_t)idx.size();
         for (int k = 0; k < t.count; ++k) {
             const int i = idx[k];
             t.w[k] = ns::Mat{G[i], update ? M[i] : nullptr, X[i], reinterpret_cast<int32_t*>(ws) + i};
         }
-        run_batch(hs[idx[0]], t, update, ws + status_bytes(count), reinterpret_cast<cudaStream_t>(stream));
-        if (engine_error()) break;
+        // (lane b % bt.lanes, whose scratch this is, is wholly on one stream)
+        run_batch(hs[idx[0]], t, update, ws + status_bytes(count) + bt.off[b], dl ? dl->lane[(b % bt.lanes) % lanes] : st);
+    }
+    if (dl) {
+        for (int l = 0; l < lanes; ++l) {
+            cudaEventRecord(dl->done[l], dl->lane[l]);
+            cudaStreamWaitEvent(st, dl->done[l], 0);
+        }
     }
     return launch_outcome();
 }
@@ -549,9 +586,7 @@ size_t orthdion_muon_workspace_bytes_grouped(const orthdion_muon_t* hs, int32_t 
     for (int i = 0; i < count; ++i)
         if (!valid(hs[i])) return 0;
     return guarded((size_t)0, [&] {
-        size_t scratch = 0;
-        make_batches(hs, count, &scratch);
-        return status_bytes(count) + scratch;
+        return status_bytes(count) + make_batches(hs, count).scratch;
     });
 }
 

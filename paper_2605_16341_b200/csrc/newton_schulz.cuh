@@ -60,54 +60,78 @@ struct PrepArgs {
     int64_t pitch, term_stride, mat_stride;      // of the image, in elements
 };
 
-// 8 entries of B at (row, col) and of the updated momentum; entries beyond the last column are zeros.
-__device__ __forceinline__ void load_buffer(const Mat& w, const PrepArgs& a, int64_t row, int64_t col, float (&b)[8], float (&m)[8]) {
+// 8 entries of G and M at (row, col) as they lie in memory; zeros beyond the last column.
+struct Raw { uint4 g[2], m[2]; };
+template <bool VEC>
+__device__ __forceinline__ void load_raw(const Mat& w, const PrepArgs& a, int64_t row, int64_t col, Raw& r) {
     const int64_t gi = row * a.ld_g + col, mi = row * a.ld_m + col;
-    float g[8];
-    if (a.vec) {
+    if (VEC) {
         if (a.g_bf16) {
-            const uint4 u = *reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(w.G) + gi);
-            g[0] = bf16lo_to_f32(u.x); g[1] = bf16hi_to_f32(u.x); g[2] = bf16lo_to_f32(u.y); g[3] = bf16hi_to_f32(u.y);
-            g[4] = bf16lo_to_f32(u.z); g[5] = bf16hi_to_f32(u.z); g[6] = bf16lo_to_f32(u.w); g[7] = bf16hi_to_f32(u.w);
+            r.g[0] = *reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(w.G) + gi);
         } else {
-            const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(w.G) + gi);
-            const float4 x = p[0], y = p[1];
-            g[0] = x.x; g[1] = x.y; g[2] = x.z; g[3] = x.w; g[4] = y.x; g[5] = y.y; g[6] = y.z; g[7] = y.w;
+            const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const float*>(w.G) + gi);
+            r.g[0] = p[0]; r.g[1] = p[1];
         }
         if (w.M) {
-            const float4* p = reinterpret_cast<const float4*>(w.M + mi);
-            const float4 x = p[0], y = p[1];
-            m[0] = x.x; m[1] = x.y; m[2] = x.z; m[3] = x.w; m[4] = y.x; m[5] = y.y; m[6] = y.z; m[7] = y.w;
+            const uint4* p = reinterpret_cast<const uint4*>(w.M + mi);
+            r.m[0] = p[0]; r.m[1] = p[1];
         }
     } else {
+        uint32_t* gw = reinterpret_cast<uint32_t*>(r.g);
+        uint32_t* mw = reinterpret_cast<uint32_t*>(r.m);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const bool in = col + e < a.cols;
-            g[e] = !in ? 0.f : a.g_bf16 ? __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(w.G)[gi + e])
-                                        : reinterpret_cast<const float*>(w.G)[gi + e];
-            m[e] = in && w.M ? w.M[mi + e] : 0.f;
+            if (a.g_bf16) {
+                const uint32_t v = in ? reinterpret_cast<const uint16_t*>(w.G)[gi + e] : 0u;
+                if (e % 2) gw[e / 2] |= v << 16;
+                else gw[e / 2] = v;
+            } else {
+                gw[e] = in ? reinterpret_cast<const uint32_t*>(w.G)[gi + e] : 0u;
+            }
+            if (w.M) mw[e] = in ? reinterpret_cast<const uint32_t*>(w.M)[mi + e] : 0u;
         }
     }
+}
+// Those 8 entries of B, and of the updated momentum.
+__device__ __forceinline__ void buffer_of(const Raw& r, const PrepArgs& a, bool momentum, float (&b)[8], float (&m)[8]) {
+    const uint32_t gw[8] = {r.g[0].x, r.g[0].y, r.g[0].z, r.g[0].w, r.g[1].x, r.g[1].y, r.g[1].z, r.g[1].w};
+    const uint32_t mw[8] = {r.m[0].x, r.m[0].y, r.m[0].z, r.m[0].w, r.m[1].x, r.m[1].y, r.m[1].z, r.m[1].w};
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        if (!w.M) { b[e] = g[e]; continue; }
+        const float g = a.g_bf16 ? (e % 2 ? bf16hi_to_f32(gw[e / 2]) : bf16lo_to_f32(gw[e / 2])) : __uint_as_float(gw[e]);
+        if (!momentum) { b[e] = g; continue; }
         // (the same instructions wherever B is formed: the same bits)
-        m[e] = __fmaf_rn(a.mu, m[e], __fmul_rn(a.rest, g[e]));
-        b[e] = a.nesterov ? __fmaf_rn(a.mu, m[e], __fmul_rn(a.rest, g[e])) : m[e];
+        m[e] = __fmaf_rn(a.mu, __uint_as_float(mw[e]), __fmul_rn(a.rest, g));
+        b[e] = a.nesterov ? __fmaf_rn(a.mu, m[e], __fmul_rn(a.rest, g)) : m[e];
     }
 }
 
-// Walks the 8-column chunks of the matrix that this block takes of `blocks`.
-template <class F>
-__device__ __forceinline__ void for_chunks(const PrepArgs& a, int block, int blocks, F f) {
+// Walks the 8-column chunks of the matrix that this block takes of `blocks`, U of them loaded before the first is used (one at a time:
+// 16 us for a sweep over a 4096 x 4096 bf16 matrix).
+template <int U, bool VEC, class F>
+__device__ __forceinline__ void for_chunks(const Mat& w, const PrepArgs& a, int block, int blocks, F f) {
     const int64_t cpr = (a.cols + 7) / 8, total = cpr * a.rows, step = (int64_t)blocks * blockDim.x;
     int64_t i = (int64_t)block * blockDim.x + threadIdx.x;
     int64_t row = i / cpr, c = i - row * cpr;
     const int64_t drow = step / cpr, dc = step - drow * cpr;
-    for (; i < total; i += step) {
-        f(row, c * 8);
-        row += drow; c += dc;
-        if (c >= cpr) { c -= cpr; ++row; }
+    while (i < total) {
+        Raw r[U];
+        int64_t rows[U], cols[U];
+        int n = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i < total) {
+                rows[u] = row; cols[u] = c * 8;
+                load_raw<VEC>(w, a, row, c * 8, r[u]);
+                n = u + 1;
+            }
+            i += step; row += drow; c += dc;
+            if (c >= cpr) { c -= cpr; ++row; }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (u < n) f(r[u], rows[u], cols[u]);
     }
 }
 
@@ -126,12 +150,22 @@ __global__ void __launch_bounds__(256) norm_kernel(const __grid_constant__ Table
     grid_dependency();
     const Mat& w = t.w[blockIdx.y];
     double sum = 0.0;
-    for_chunks(a, blockIdx.x, a.parts, [&](int64_t row, int64_t col) {
+    auto add = [&](const Raw& r, int64_t, int64_t) {
         float b[8], m[8];
-        load_buffer(w, a, row, col, b, m);
+        buffer_of(r, a, w.M != nullptr, b, m);
+        // eight squares in 32 bits (2^-22 of them at most), unless they overflow or come near what vanishes
+        float q = b[0] * b[0];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum = fma((double)b[e], (double)b[e], sum);
-    });
+        for (int e = 1; e < 8; ++e) q = fmaf(b[e], b[e], q);
+        if (q >= 1e-28f && q <= 1e38f) {
+            sum += (double)q;
+        } else {
+#pragma unroll 1
+            for (int e = 0; e < 8; ++e) sum = fma((double)b[e], (double)b[e], sum);
+        }
+    };
+    if (a.vec) for_chunks<4, true>(w, a, blockIdx.x, a.parts, add);
+    else for_chunks<2, false>(w, a, blockIdx.x, a.parts, add);
     sum = block_sum(sum, red);
     if (threadIdx.x == 0) a.part[(int64_t)blockIdx.y * MAX_PARTS + blockIdx.x] = sum;
 }
@@ -162,9 +196,9 @@ __global__ void __launch_bounds__(256) prep_kernel(const __grid_constant__ Table
     }
     if (!finite) return;
     __half* img = a.img + (int64_t)blockIdx.y * a.mat_stride;
-    for_chunks(a, blockIdx.x, gridDim.x, [&](int64_t row, int64_t col) {
+    auto write = [&](const Raw& r, int64_t row, int64_t col) {
         float b[8], m[8];
-        load_buffer(w, a, row, col, b, m);
+        buffer_of(r, a, w.M != nullptr, b, m);
         if (w.M) {
             float* dst = w.M + row * a.ld_m + col;
             if (a.vec) {
@@ -190,7 +224,9 @@ __global__ void __launch_bounds__(256) prep_kernel(const __grid_constant__ Table
             }
             *reinterpret_cast<uint4*>(dst + a.term_stride) = half8(b, 1.f);
         }
-    });
+    };
+    if (a.vec) for_chunks<4, true>(w, a, blockIdx.x, gridDim.x, write);
+    else for_chunks<2, false>(w, a, blockIdx.x, gridDim.x, write);
 }
 
 // ---- products between images ---------------------------------------------------------------------
@@ -214,12 +250,11 @@ struct GemmArgs {
     int64_t pitch, term_stride, mat_stride;
     Slot* slot;
     int32_t count;
-    int32_t update, x_bf16;                   // EPI_FINAL: X <- wc X - wd D, or X <- D
+    int32_t update, x_bf16, x_vec;            // EPI_FINAL: X <- wc X - wd D, or X <- D; x_vec: rows of X on 16-byte boundaries, and whole vectors
     float wc, wd;
     int64_t ld_x;
     alignas(64) CUtensorMap map_a;
     alignas(64) CUtensorMap map_b;
-    alignas(64) CUtensorMap map_out;
 };
 struct NoTable { int32_t unused; };
 
@@ -240,13 +275,6 @@ __device__ __forceinline__ void tma_load4(uint32_t dst, const CUtensorMap* map, 
             "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
             ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(row), "r"(term), "r"(mat), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void tma_store4(const CUtensorMap* map, uint32_t src, int x, int row, int term, int mat) {
-    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];"
-                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(src), "r"(x), "r"(row), "r"(term), "r"(mat) : "memory");
-    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-}
-__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&v)[32]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
@@ -257,6 +285,13 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&v)[32]) {
           "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
         : "r"(taddr) : "memory");
 }
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const float* v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+        ::"r"(taddr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]),
+          "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Rows of a result tile, and rows of B that one CTA holds of it.
 template <bool PAIR> __host__ __device__ constexpr int tile_rows() { return PAIR ? 256 : 128; }
@@ -298,6 +333,173 @@ __device__ __forceinline__ Tile decode(const GemmArgs& g, int t) {
     return r;
 }
 
+// The rows of one warp (row_w + lane) and NC columns from col_w of a result in tensor memory at d -> image, 32 columns at a time,
+// through shared memory so that four lanes write 64 bytes of a row; with `mirror` also to the mirrored place, where pairs of rows and
+// columns are exchanged between neighbouring lanes first.  (With TMA stores out of two such blocks in turn a block took 1200 cycles,
+// most of them the wait until the one before was read, and its mirror image in 4-byte stores as long again.)
+template <int TERMS, int NC>
+__device__ __forceinline__ void image_epilogue(const GemmArgs& g, uint32_t d, float alpha, int mat, int row_w, int lane, int col_w, bool mirror,
+                                               unsigned char* stage_ptr) {
+    const int row = row_w + lane;
+    const int64_t base = mat * g.mat_stride;
+    const __half* add = g.add ? g.add + base + (int64_t)min(row, g.rows - 1) * g.pitch : nullptr;
+    const int sr = lane / 4, sc = lane % 4;              // row and 16-byte chunk that this lane moves out
+    const bool odd = lane & 1;
+    unsigned char* mir_ptr = stage_ptr + 2048;
+    uint4 cq[TERMS][4];
+    auto fetch = [&](int col) {
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) cq[t][i] = *reinterpret_cast<const uint4*>(add + t * g.term_stride + col + i * 8);
+    };
+    if (add) fetch(col_w);
+#pragma unroll 1
+    for (int q = 0; q < NC / 32; ++q) {
+        const int col = col_w + q * 32;
+        if (col >= g.cols) break;
+        float v[32];
+        {
+            uint32_t u[32];
+            tmem_ld32(d + q * 32, u);
+            tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] = alpha * __uint_as_float(u[e]);
+        }
+        if (add) {
+#pragma unroll
+            for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t h[4] = {cq[t][i].x, cq[t][i].y, cq[t][i].z, cq[t][i].w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[k]));
+                        v[i * 8 + 2 * k] = fmaf(g.beta, f.x, v[i * 8 + 2 * k]);
+                        v[i * 8 + 2 * k + 1] = fmaf(g.beta, f.y, v[i * 8 + 2 * k + 1]);
+                    }
+                }
+            if (col == row_w) {          // the block on the diagonal
+#pragma unroll
+                for (int e = 0; e < 32; ++e) v[e] += e == lane ? g.diag : 0.f;
+            }
+            if (q + 1 < NC / 32 && col + 32 < g.cols) fetch(col + 32);
+        }
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t) {
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t h[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    float &x = v[i * 8 + 2 * k], &y = v[i * 8 + 2 * k + 1];
+                    h[k] = pack_f16x2(x, y);
+                    if (TERMS == 2 && t == 0) {
+                        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[k]));
+                        x -= f.x; y -= f.y;
+                    }
+                    if (mirror) {
+                        // an even lane gets its neighbour's entry of the first column, an odd one that of the second
+                        const uint32_t o = __shfl_xor_sync(0xffffffffu, h[k], 1);
+                        *reinterpret_cast<uint32_t*>(mir_ptr + (i * 8 + 2 * k + odd) * 64 + (lane - odd) * 2) =
+                            odd ? __byte_perm(o, h[k], 0x7632) : __byte_perm(h[k], o, 0x5410);
+                    }
+                }
+                *reinterpret_cast<uint4*>(stage_ptr + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+            }
+            __syncwarp();
+            __half* out = g.out + base + t * g.term_stride;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = sr + 8 * i;
+                if (row_w + r < g.rows && col + sc * 8 < g.cols)
+                    *reinterpret_cast<uint4*>(out + (int64_t)(row_w + r) * g.pitch + col + sc * 8) =
+                        *reinterpret_cast<const uint4*>(stage_ptr + r * 64 + ((sc ^ ((r >> 1) & 3)) << 4));
+                if (mirror && col + r < g.cols && row_w + sc * 8 < g.rows)
+                    *reinterpret_cast<uint4*>(out + (int64_t)(col + r) * g.pitch + row_w + sc * 8) = *reinterpret_cast<const uint4*>(mir_ptr + r * 64 + sc * 16);
+            }
+        }
+    }
+}
+
+// The same rows and columns -> the caller's matrix, along rows: 8 entries a lane where rows start on 16-byte boundaries.
+template <class T, int NC>
+__device__ __forceinline__ void final_epilogue(const GemmArgs& g, uint32_t d, float alpha, void* X, int row_w, int lane, int col_w, unsigned char* stage_ptr) {
+    float* blk = reinterpret_cast<float*>(stage_ptr);
+    const int high = min(32, g.rows - row_w);
+    constexpr int V = 16 / sizeof(T), PER = 32 / V, STEP = 32 / PER;      // entries a lane takes, lanes a row, rows a turn
+    const int vr = lane / PER, vc = (lane % PER) * V;
+    uint4 old[32 / STEP];
+    auto fetch = [&](int col) {
+#pragma unroll
+        for (int i = 0; i < 32 / STEP; ++i) {
+            const int r = vr + i * STEP;
+            if (r < high && col + vc < g.cols) old[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(X) + (int64_t)(row_w + r) * g.ld_x + col + vc);
+        }
+    };
+    if (g.x_vec && g.update) fetch(col_w);
+#pragma unroll 1
+    for (int q = 0; q < NC / 32; ++q) {
+        const int col = col_w + q * 32;
+        if (col >= g.cols) break;
+        {
+            uint32_t u[32];
+            tmem_ld32(d + q * 32, u);
+            tmem_ld_wait();
+            __syncwarp();
+            // rows of 32, four-entry groups exchanged within a row so that neither side meets a bank twice
+#pragma unroll
+            for (int e = 0; e < 32; e += 4)
+                *reinterpret_cast<float4*>(blk + lane * 32 + (e ^ ((lane & 7) * 4))) =
+                    make_float4(alpha * __uint_as_float(u[e]), alpha * __uint_as_float(u[e + 1]), alpha * __uint_as_float(u[e + 2]), alpha * __uint_as_float(u[e + 3]));
+            __syncwarp();
+        }
+        if (g.x_vec) {
+#pragma unroll
+            for (int i = 0; i < 32 / STEP; ++i) {
+                const int r = vr + i * STEP;
+                if (r >= high || col + vc >= g.cols) continue;
+                float v[V];
+#pragma unroll
+                for (int e = 0; e < V; e += 4) {
+                    const float4 f = *reinterpret_cast<const float4*>(blk + r * 32 + ((vc + e) ^ ((r & 7) * 4)));
+                    v[e] = f.x; v[e + 1] = f.y; v[e + 2] = f.z; v[e + 3] = f.w;
+                }
+                if (g.update) {
+                    const uint32_t w[4] = {old[i].x, old[i].y, old[i].z, old[i].w};
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const float x = sizeof(T) == 4 ? __uint_as_float(w[e * 4 / V]) : e % 2 ? bf16hi_to_f32(w[e / 2]) : bf16lo_to_f32(w[e / 2]);
+                        v[e] = g.wc * x - g.wd * v[e];
+                    }
+                }
+                T* x = reinterpret_cast<T*>(X) + (int64_t)(row_w + r) * g.ld_x + col + vc;
+                if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(x) = make_float4(v[0], v[1], v[2], v[3]);
+                else *reinterpret_cast<uint4*>(x) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+            }
+            if (g.update && q + 1 < NC / 32) fetch(col + 32);
+        } else if (col + lane < g.cols) {
+            T* x = reinterpret_cast<T*>(X) + (int64_t)row_w * g.ld_x + col + lane;
+            // (sixteen loads under way: stores to X in between would hold each of them back)
+#pragma unroll 1
+            for (int r0 = 0; r0 < high; r0 += 16) {
+                float x0[16];
+                if (g.update) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) x0[r] = r0 + r < high ? to_float(x[(r0 + r) * g.ld_x]) : 0.f;
+                }
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float f = blk[(r0 + r) * 32 + (lane ^ ((r & 7) * 4))];
+                    if (r0 + r < high) x[(r0 + r) * g.ld_x] = from_float<T>(g.update ? g.wc * x0[r] - g.wd * f : f);
+                }
+            }
+        }
+        __syncwarp();
+    }
+}
+
 template <bool PAIR, int BN, int TERMS, int EPI, class TABLE>
 __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant__ TABLE table, const __grid_constant__ GemmArgs g) {
     constexpr int NB = side_rows<PAIR, BN>(), STAGE = stage_bytes<PAIR, BN, TERMS>(), NS = stages<PAIR, BN, TERMS>();
@@ -310,7 +512,6 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
     unsigned char* smem = smem_raw + (base - raw);
-    const uint32_t staging0 = base + STAGE_BYTES;
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + STAGE_BYTES + 8 * 4096);
     const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * MAX_STAGES, tfull0 = empty0 + 8 * MAX_STAGES, tempty0 = tfull0 + 16;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * MAX_STAGES + 4);
@@ -325,7 +526,6 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
         fence_async_smem();
         prefetch_tensor_map(&g.map_a);
         prefetch_tensor_map(&g.map_b);
-        if (EPI == EPI_IMAGE) prefetch_tensor_map(&g.map_out);
     }
     if (warp == 1) {
         if (PAIR) tmem_alloc_pair(smem_u32(tmem_slot), 2 * BN);
@@ -415,144 +615,71 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
     } else {
         // ---------------- epilogue: warp w has the 32 rows that its tensor-memory quarter holds, and half the columns ----------------
         const int quarter = warp % 4, half = (warp - 2) / 4;
-        const uint32_t staging = staging0 + (uint32_t)(warp - 2) * 4096u;
         unsigned char* stage_ptr = smem + STAGE_BYTES + (warp - 2) * 4096;
         int acc = 0; uint32_t aph = 0;
         bool ok = true;
         for (int t = tile0; t < g.total && ok; t += tstep) {
             const Tile c = decode<PAIR, BN>(g, t);
             if (!c.active) continue;
-            float v[NC];
-            for (int k0 = 0; k0 < g.kblocks; k0 += g.chunk) {
+            const int row_w = c.row0 + crank * 128 + quarter * 32, col_w = c.col0 + half * NC;
+            const bool mine = row_w < g.rows && col_w < g.cols;
+            const uint32_t mine_tmem = tmem_base + half * NC + ((uint32_t)(quarter * 32) << 16);
+            if (TERMS == 1) {
                 // (all lanes alike: a wait that ran out for one ends the warp's work)
                 ok = __all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * acc, aph, abort_flag));
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t d = tmem_base + acc * BN + half * NC + ((uint32_t)(quarter * 32) << 16);
+            } else {
+                // Sums of the chunks, in registers; the total goes back to where the last chunk was, so that what follows is one
+                // rolled loop for either form (unrolled, its code is fetched more slowly than it runs).
+                float v[NC];
 #pragma unroll
-                for (int q = 0; q < NC / 16; ++q) {
-                    uint32_t u[16];
-                    tmem_ld16(d + q * 16, u);
-                    tmem_ld_wait();
+                for (int e = 0; e < NC; ++e) v[e] = 0.f;
+                int left = (g.kblocks + g.chunk - 1) / g.chunk;
+                while (true) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * acc, aph, abort_flag));
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t d = mine_tmem + acc * BN;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) v[q * 16 + e] = (TERMS == 2 && k0 > 0) ? v[q * 16 + e] + __uint_as_float(u[e]) : __uint_as_float(u[e]);
+                    for (int q = 0; q < NC / 16; ++q) {
+                        uint32_t u[16];
+                        tmem_ld16(d + q * 16, u);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) v[q * 16 + e] += __uint_as_float(u[e]);
+                    }
+                    if (--left == 0) break;
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) { if (PAIR) mbar_arrive_remote(tempty_ld + 8 * acc); else mbar_arrive(tempty0 + 8 * acc); }
+                    if (++acc == 2) { acc = 0; aph ^= 1; }
                 }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) { if (PAIR) mbar_arrive_remote(tempty_ld + 8 * acc); else mbar_arrive(tempty0 + 8 * acc); }
-                if (++acc == 2) { acc = 0; aph ^= 1; }
+                if (!ok) break;
+                const uint32_t d = mine_tmem + acc * BN;
+#pragma unroll
+                for (int q = 0; q < NC / 16; ++q) tmem_st16(d + q * 16, &v[q * 16]);
+                tmem_st_wait();
             }
-            if (!ok) break;
-            const int row_w = c.row0 + crank * 128 + quarter * 32, row = row_w + lane;
-            const int col_w = c.col0 + half * NC;
+            const uint32_t d = mine_tmem + acc * BN;
             float alpha = g.alpha;
             if (g.sigma_pow) {
                 const float sg = g.slot[c.mat].sigma;
                 alpha *= g.sigma_pow == 2 ? sg * sg : sg;
             }
-            if (row_w >= g.rows) continue;
             if constexpr (EPI == EPI_IMAGE) {
-#pragma unroll
-                for (int q = 0; q < NC / 64; ++q) {
-                    const int col = col_w + q * 64;
-                    if (col < g.cols) {
-#pragma unroll
-                        for (int e = 0; e < 64; ++e) v[q * 64 + e] *= alpha;
-                        if (g.add) {
-                            if (row < g.rows) {
-                                const __half* src = g.add + c.mat * g.mat_stride + (int64_t)row * g.pitch + col;
-#pragma unroll
-                                for (int term = 0; term < TERMS; ++term)
-#pragma unroll
-                                    for (int e = 0; e < 64; e += 8) {
-                                        const uint4 u = *reinterpret_cast<const uint4*>(src + term * g.term_stride + e);
-                                        const uint32_t h[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-                                        for (int i = 0; i < 4; ++i) {
-                                            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
-                                            v[q * 64 + e + 2 * i] += g.beta * f.x;
-                                            v[q * 64 + e + 2 * i + 1] += g.beta * f.y;
-                                        }
-                                    }
-                            }
-                            if (col + 64 > row_w && col < row_w + 32) {
-#pragma unroll
-                                for (int e = 0; e < 64; ++e) v[q * 64 + e] += col + e == row ? g.diag : 0.f;
-                            }
-                        }
-#pragma unroll
-                        for (int term = 0; term < TERMS; ++term) {
-                            bulk_wait_read();
-                            __syncwarp();
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                uint32_t h[4];
-#pragma unroll
-                                for (int k = 0; k < 4; ++k) {
-                                    float &x = v[q * 64 + i * 8 + 2 * k], &y = v[q * 64 + i * 8 + 2 * k + 1];
-                                    h[k] = pack_f16x2(x, y);
-                                    if (c.mirror) {
-                                        __half* m = g.out + c.mat * g.mat_stride + term * g.term_stride + (int64_t)(col + i * 8 + 2 * k) * g.pitch + row;
-                                        const __half2 hh = *reinterpret_cast<const __half2*>(&h[k]);
-                                        if (row < g.rows) {
-                                            if (col + i * 8 + 2 * k < g.cols) m[0] = __low2half(hh);
-                                            if (col + i * 8 + 2 * k + 1 < g.cols) m[g.pitch] = __high2half(hh);
-                                        }
-                                    }
-                                    if (TERMS == 2 && term == 0) {
-                                        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[k]));
-                                        x -= f.x; y -= f.y;
-                                    }
-                                }
-                                *reinterpret_cast<uint4*>(stage_ptr + lane * 128 + ((i ^ (lane & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
-                            }
-                            fence_async_smem();
-                            __syncwarp();
-                            if (lane == 0) tma_store4(&g.map_out, staging, col, row_w, term, c.mat);
-                        }
-                    }
-                }
+                if (mine) image_epilogue<TERMS, NC>(g, d, alpha, c.mat, row_w, lane, col_w, c.mirror, stage_ptr);
             } else {
-                const Mat& w = table.w[c.mat];
-                if (g.slot[c.mat].status) continue;
-                float* blk = reinterpret_cast<float*>(stage_ptr);
-#pragma unroll
-                for (int q = 0; q < NC / 32; ++q) {
-                    const int col = col_w + q * 32;
-                    if (col < g.cols) {
-                        // through shared memory, so that the lanes run along a row
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) blk[lane * 32 + (e ^ lane)] = v[q * 32 + e] * alpha;
-                        __syncwarp();
-                        const int cl = col + lane, high = min(32, g.rows - row_w);
-                        if (cl < g.cols) {
-                            const int64_t at = (int64_t)row_w * g.ld_x + cl;
-                            auto rows16 = [&](auto* x) {
-                                using T = std::remove_pointer_t<decltype(x)>;
-                                // (sixteen loads under way: stores to X in between would hold each of them back)
-#pragma unroll 1
-                                for (int r0 = 0; r0 < high; r0 += 16) {
-                                    float old[16];
-                                    if (g.update) {
-#pragma unroll
-                                        for (int r = 0; r < 16; ++r) old[r] = r0 + r < high ? to_float(x[(r0 + r) * g.ld_x]) : 0.f;
-                                    }
-#pragma unroll
-                                    for (int r = 0; r < 16; ++r) {
-                                        const float d = blk[(r0 + r) * 32 + (lane ^ (r0 + r))];
-                                        if (r0 + r < high) x[(r0 + r) * g.ld_x] = from_float<T>(g.update ? g.wc * old[r] - g.wd * d : d);
-                                    }
-                                }
-                            };
-                            if (g.x_bf16) rows16(reinterpret_cast<__nv_bfloat16*>(w.X) + at);
-                            else rows16(reinterpret_cast<float*>(w.X) + at);
-                        }
-                        __syncwarp();
-                    }
+                if (mine && !g.slot[c.mat].status) {
+                    if (g.x_bf16) final_epilogue<__nv_bfloat16, NC>(g, d, alpha, table.w[c.mat].X, row_w, lane, col_w, stage_ptr);
+                    else final_epilogue<float, NC>(g, d, alpha, table.w[c.mat].X, row_w, lane, col_w, stage_ptr);
                 }
             }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) { if (PAIR) mbar_arrive_remote(tempty_ld + 8 * acc); else mbar_arrive(tempty0 + 8 * acc); }
+            if (++acc == 2) { acc = 0; aph ^= 1; }
         }
-        if (EPI == EPI_IMAGE) bulk_wait();
     }
 
     // ---------------- teardown ----------------
