@@ -12,7 +12,6 @@
 #include <vector>
 
 #include "adamw.cuh"
-#include "lanes.cuh"
 #include "newton_schulz.cuh"
 
 using namespace od;
@@ -20,9 +19,7 @@ using namespace od;
 namespace {
 constexpr uint32_t kMuonMagic = 0x0D10B0E5u, kAdamWMagic = 0x0D10ADA3u;
 constexpr int32_t kMaxSteps = 32;
-constexpr size_t kScratchBudget = (size_t)1 << 30;     // per launch batch
-constexpr int kPlannedLanes = 4;
-constexpr int kTwoTermChunk = 1;                        // depth blocks of 64 that two-plane products sum in tensor memory
+constexpr size_t kScratchBudget = (size_t)4 << 30;     // per launch
 }  // namespace
 
 struct orthdion_muon_plan {
@@ -78,20 +75,17 @@ int terms_of(const orthdion_muon_plan* p) { return p->passes == 3 ? 2 : 1; }
 // the norm) and not in the last two, but in between (noise and 32 strong directions, 129 x 1000, error of the result by grouping of five steps:
 // 2,2,1 8.1e-3; 1,2,2 2.8e-3; singles 2.5e-3; 2,1,2 2.3e-3; 2,1,1,1 2.2e-3).  A pair in front costs a square matrix nothing and saves
 // a rounding of X; one at the end pays where the matrix is longer than wide.
-std::vector<int> group_steps(const orthdion_muon_plan* p) {
-    std::vector<int> out;
+struct Groups { int32_t pair_first, pair_last; };
+Groups group_steps(const orthdion_muon_plan* p) {
     const int64_t s = std::min(p->m, p->n), l = std::max(p->m, p->n);
-    const bool pair_last = p->steps >= 5 && 4 * l >= 5 * s;
-    for (int left = p->steps; left > 0; left -= out.back())
-        out.push_back((left == p->steps || (pair_last && left == 2)) ? std::min(2, left) : 1);
-    return out;
+    return Groups{p->steps >= 2, p->steps >= 5 && 4 * l >= 5 * s};
 }
 
+// The scratch of `count` matrices of one plan: byte offsets, strides in elements.
 struct Scratch {
-    int64_t slot, part, x[2], sq[4];        // byte offsets inside the scratch of a batch of `count` matrices
-    int64_t x_pitch, x_term, x_mat;         // in elements
-    int64_t s_pitch, s_term, s_mat;
-    size_t bytes;
+    size_t slot, part, tile_done, x[2], sq[4], bytes;
+    int32_t tiles_sq, tiles_x, counts;
+    int64_t x_pitch, x_term, x_mat, s_pitch, s_term, s_mat;
 };
 
 Scratch scratch_layout(const orthdion_muon_plan* p, int count) {
@@ -100,252 +94,222 @@ Scratch scratch_layout(const orthdion_muon_plan* p, int count) {
     const int64_t s = std::min(p->m, p->n);
     c.x_pitch = (int64_t)align_up(p->n, 64); c.x_term = p->m * c.x_pitch; c.x_mat = terms * c.x_term;
     c.s_pitch = (int64_t)align_up(s, 64); c.s_term = s * c.s_pitch; c.s_mat = terms * c.s_term;
-    const std::vector<int> groups = group_steps(p);
+    const Groups g = group_steps(p);
     size_t off = 0;
     c.slot = 0; off += align_up(count * sizeof(ns::Slot), 256);
-    c.part = off; off += align_up((size_t)count * ns::MAX_PARTS * 8, 256);
+    c.part = off; off += align_up((size_t)count * ns::MAX_PARTS * 8, 1024);
+    const int64_t st = ns::tiles_along((int)s);
+    c.tiles_sq = (int32_t)(st * (st + 1) / 2);
+    c.tiles_x = ns::tiles_along((int)p->m) * ns::tiles_along((int)p->n);
+    c.counts = 4 * c.tiles_sq + 2 * c.tiles_x;
+    c.tile_done = off; off += align_up((size_t)count * c.counts * 4, 1024);
     for (int i = 0; i < 2; ++i) {
         c.x[i] = off;
-        if (i == 0 || groups.size() > 1) off += align_up((size_t)count * c.x_mat * 2, 1024);
+        if (i == 0 || p->steps > 1 + g.pair_first) off += align_up((size_t)count * c.x_mat * 2, 1024);
     }
     for (int i = 0; i < 4; ++i) {
         c.sq[i] = off;
-        if (i < 2 || groups[0] > 1) off += align_up((size_t)count * c.s_mat * 2, 1024);
+        if (i < 2 || g.pair_first) off += align_up((size_t)count * c.s_mat * 2, 1024);
     }
     c.bytes = align_up(off, 1024);
     return c;
 }
 
-// Launch batches of a call (matrices of one class, so many that the scratch stays within the budget), in the order in which they are
-// enqueued, and the lanes they run on: one chain of launches leaves multiprocessors idle at the end of each, which those of another lane fill.
-// Every lane has scratch of its own.
-struct Batching {
-    std::vector<std::vector<int>> batches;
-    std::vector<size_t> off;           // scratch offset
-    int lanes = 1;                     // batch i runs on lane i % lanes
-    size_t scratch = 0;
-};
-
-double cost(const orthdion_muon_plan* p, size_t count) {
+double cost(const orthdion_muon_plan* p) {
     const double s = (double)std::min(p->m, p->n), l = (double)std::max(p->m, p->n);
-    return (double)count * p->steps * s * s * (3 * l + s) * (p->passes == 3 ? 3 : 1);
+    return p->steps * s * s * (3 * l + s) * (p->passes == 3 ? 3 : 1);
 }
 
-Batching make_batches(const orthdion_muon_t* hs, int32_t count) {
-    Batching out;
+// The launches of a call: matrices of up to MAX_CLASSES plans that are worked on together, as many as the scratch budget holds.
+struct Launch {
+    std::vector<std::vector<int>> classes;     // matrices of one plan each
+    std::vector<size_t> off;                   // their scratch
+    size_t bytes = 0;
+    int matrices = 0;
+};
+
+std::vector<Launch> make_launches(const orthdion_muon_t* hs, int32_t count, size_t* scratch) {
+    std::vector<std::vector<int>> classes;
     std::vector<char> done(count, 0);
     for (int i = 0; i < count; ++i) {
         if (done[i]) continue;
-        std::vector<int> cls;
+        classes.emplace_back();
         for (int j = i; j < count; ++j)
-            if (!done[j] && same_class(hs[i], hs[j])) { cls.push_back(j); done[j] = 1; }
-        const size_t per = scratch_layout(hs[i], 1).bytes;
-        const size_t cap = std::min<size_t>(std::max<size_t>(1, kScratchBudget / per), ns::MAX_BATCH);
-        const size_t nb = (cls.size() + cap - 1) / cap, bs = (cls.size() + nb - 1) / nb;
-        for (size_t b = 0; b < cls.size(); b += bs) out.batches.emplace_back(cls.begin() + b, cls.begin() + std::min(cls.size(), b + bs));
+            if (!done[j] && same_class(hs[i], hs[j])) { classes.back().push_back(j); done[j] = 1; }
     }
-    // heaviest first
-    std::stable_sort(out.batches.begin(), out.batches.end(),
-                     [&](const auto& a, const auto& b) { return cost(hs[a[0]], a.size()) > cost(hs[b[0]], b.size()); });
-    out.lanes = std::min<int>(kPlannedLanes, (int)out.batches.size());
-    std::vector<size_t> most(out.lanes, 0), at(out.lanes, 0);
-    for (size_t b = 0; b < out.batches.size(); ++b)
-        most[b % out.lanes] = std::max(most[b % out.lanes], scratch_layout(hs[out.batches[b][0]], (int)out.batches[b].size()).bytes);
-    for (int l = 0; l < out.lanes; ++l) { at[l] = out.scratch; out.scratch += most[l]; }
-    for (size_t b = 0; b < out.batches.size(); ++b) out.off.push_back(at[b % out.lanes]);
+    // one-term and two-term products are kernels of their own; the heaviest matrices first, so that the light ones fill what they leave
+    std::stable_sort(classes.begin(), classes.end(), [&](const auto& a, const auto& b) {
+        const orthdion_muon_plan *p = hs[a[0]], *q = hs[b[0]];
+        return terms_of(p) != terms_of(q) ? terms_of(p) > terms_of(q) : cost(p) > cost(q);
+    });
+    std::vector<Launch> out;
+    int terms = 0;
+    for (const auto& cls : classes) {
+        const orthdion_muon_plan* p = hs[cls[0]];
+        for (size_t at = 0; at < cls.size();) {
+            if (out.empty() || terms != terms_of(p) || out.back().classes.size() == ns::MAX_CLASSES || out.back().matrices == ns::MAX_BATCH ||
+                out.back().bytes + scratch_layout(p, 1).bytes > kScratchBudget)
+                out.emplace_back();
+            terms = terms_of(p);
+            Launch& l = out.back();
+            size_t n = std::min<size_t>(cls.size() - at, ns::MAX_BATCH - l.matrices);
+            while (n > 1 && l.bytes + scratch_layout(p, (int)n).bytes > kScratchBudget) --n;
+            l.classes.emplace_back(cls.begin() + at, cls.begin() + at + n);
+            l.off.push_back(l.bytes);
+            l.bytes += scratch_layout(p, (int)n).bytes;
+            l.matrices += (int)n;
+            at += n;
+        }
+    }
+    *scratch = 0;
+    for (const Launch& l : out) *scratch = std::max(*scratch, l.bytes);
     return out;
 }
 
 size_t status_bytes(int32_t count) { return align_up((size_t)count * 4, 1024); }
 
-// A 4-d map over the images (columns, rows, planes, matrices) of a batch.
-bool encode(CUtensorMap* map, const void* base, int64_t cols, int64_t rows, int terms, int count, int64_t pitch, int64_t term, int64_t mat,
-            int box_rows, int box_terms) {
+// Maps over the images of a class: (columns, rows, planes, matrices) in boxes of 64 x 128, and (64 columns, rows, groups of 64 columns,
+// planes, matrices) in boxes of two groups of 64 rows.
+void encode(CUtensorMap* k, CUtensorMap* mn, const void* base, int64_t cols, int64_t rows, int terms, int count, int64_t pitch, int64_t term, int64_t mat) {
     TensorMapEncodeFn enc = tensor_map_encoder();
-    if (!enc) { engine_error() = 1; return false; }
-    const cuuint64_t dims[4] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)terms, (cuuint64_t)count};
-    const cuuint64_t strides[3] = {(cuuint64_t)pitch * 2, (cuuint64_t)term * 2, (cuuint64_t)mat * 2};
-    const cuuint32_t box[4] = {64, (cuuint32_t)box_rows, (cuuint32_t)box_terms, 1}, ones[4] = {1, 1, 1, 1};
-    const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) {
-        std::fprintf(stderr, "orthdion: cuTensorMapEncodeTiled failed (%d)\n", (int)r);
-        engine_error() = 2;
-        return false;
-    }
-    return true;
-}
-
-struct Image {
-    char* base;
-    int64_t rows, cols, pitch, term, mat;
-};
-
-// One batch on its way through the products.
-struct Chain {
-    const orthdion_muon_plan* p;
-    int count, terms;
-    ns::Slot* slot;
-    cudaStream_t st;
-};
-
-template <bool PAIR, int BN, int TERMS, int EPI, class TABLE>
-void launch_gemm(const Chain& c, ns::GemmArgs& g, const Image& a, const Image& b, const Image* out, const TABLE& table) {
-    constexpr int TM = ns::tile_rows<PAIR>(), NB = ns::side_rows<PAIR, BN>();
-    g.m_tiles = (g.rows + TM - 1) / TM;
-    g.n_tiles = (g.cols + BN - 1) / BN;
-    g.tiles = g.sym ? (TM / BN == 1 ? g.m_tiles * (g.m_tiles + 1) / 2 : g.m_tiles * (g.m_tiles + 1)) : g.m_tiles * g.n_tiles;
-    g.total = g.tiles * c.count;
-    if (!encode(&g.map_a, a.base, a.cols, a.rows, TERMS, c.count, a.pitch, a.term, a.mat, g.a_mn ? 64 : 128, TERMS)) return;
-    if (!encode(&g.map_b, b.base, b.cols, b.rows, TERMS, c.count, b.pitch, b.term, b.mat, g.b_mn ? 64 : NB, TERMS)) return;
-    if (out) {
-        g.out = reinterpret_cast<__half*>(out->base);
-        g.pitch = out->pitch; g.term_stride = out->term; g.mat_stride = out->mat;
-    }
-    const int sms = sm_count(), units = std::min(g.total, PAIR ? sms / 2 : sms);
-    launch(ns::gemm_kernel<PAIR, BN, TERMS, EPI, TABLE>, dim3((unsigned)(PAIR ? 2 * units : units)), ns::THREADS, ns::SMEM_BYTES, PAIR ? 2 : 1,
-           prof::S_NS_PRODUCT, c.st, table, g);
-}
-
-// Tile shape of a product.
-enum TileShape { T_PAIR256, T_SINGLE128 };
-TileShape tile_shape(const ns::GemmArgs& g, int count) {
-    const int64_t mt = (g.rows + 255) / 256, nt = (g.cols + 255) / 256;
-    const int64_t tiles = (g.sym ? mt * (mt + 1) / 2 : mt * nt) * count;
-    return tiles >= sm_count() / 2 ? T_PAIR256 : T_SINGLE128;
-}
-
-template <int EPI, class TABLE>
-void product(const Chain& c, ns::GemmArgs& g, const Image& a, const Image& b, const Image* out, const TABLE& table) {
-    g.slot = c.slot; g.count = c.count;
-    g.chunk = c.terms == 2 ? kTwoTermChunk : g.kblocks;
-    const TileShape ts = tile_shape(g, c.count);
-    if (c.terms == 2) {
-        if (ts == T_PAIR256) launch_gemm<true, 256, 2, EPI>(c, g, a, b, out, table);
-        else launch_gemm<false, 128, 2, EPI>(c, g, a, b, out, table);
-    } else {
-        if (ts == T_PAIR256) launch_gemm<true, 256, 1, EPI>(c, g, a, b, out, table);
-        else launch_gemm<false, 128, 1, EPI>(c, g, a, b, out, table);
-    }
-}
-
-int depth_blocks(int64_t k) { return (int)((k + 63) / 64); }
-
-// out = alpha A B (+ beta C + diag I) of symmetric s x s images that commute
-void square_product(const Chain& c, const Image& a, const Image& b, const Image& out, float alpha, const Image* add = nullptr, float beta = 0.f,
-                    float diag = 0.f) {
-    ns::GemmArgs g{};
-    g.rows = g.cols = (int32_t)a.rows;
-    g.kblocks = depth_blocks(a.rows);
-    g.sym = 1;
-    g.alpha = alpha; g.beta = beta; g.diag = diag;
-    g.add = add ? reinterpret_cast<const __half*>(add->base) : nullptr;
-    product<ns::EPI_IMAGE>(c, g, a, b, &out, ns::NoTable{0});
-}
-
-// A = X X^T, or X^T X of a tall matrix
-void gram_product(const Chain& c, const Image& x, const Image& out, bool first) {
-    const bool wide = c.p->m <= c.p->n;
-    ns::GemmArgs g{};
-    g.rows = g.cols = (int32_t)std::min(c.p->m, c.p->n);
-    g.kblocks = depth_blocks(std::max(c.p->m, c.p->n));
-    g.sym = 1;
-    g.a_mn = g.b_mn = wide ? 0 : 1;
-    g.alpha = 1.f / ns::UNIT;
-    g.sigma_pow = first ? 2 : 0;
-    product<ns::EPI_IMAGE>(c, g, x, x, &out, ns::NoTable{0});
-}
-
-// X' = P X, or X P of a tall matrix: to an image, or (out null) to the caller's matrix
-void apply_product(const Chain& c, const Image& pm, const Image& x, const Image* out, bool first, const ns::Table* table, bool update) {
-    const bool wide = c.p->m <= c.p->n;
-    ns::GemmArgs g{};
-    g.rows = (int32_t)c.p->m; g.cols = (int32_t)c.p->n;
-    g.kblocks = depth_blocks(std::min(c.p->m, c.p->n));
-    g.b_mn = wide ? 1 : 0;
-    g.sigma_pow = first ? 1 : 0;
-    const Image &a = wide ? pm : x, &b = wide ? x : pm;
-    if (out) {
-        g.alpha = 1.f / ns::UNIT;
-        product<ns::EPI_IMAGE>(c, g, a, b, out, ns::NoTable{0});
-    } else {
-        g.alpha = 1.f / (ns::UNIT * ns::UNIT);
-        g.update = update;
-        g.x_bf16 = c.p->x_dtype == ORTHDION_DTYPE_BF16;
-        g.wc = 1.f - c.p->eta * c.p->wd; g.wd = c.p->eta * c.p->scale;
-        g.ld_x = c.p->ld_x;
-        const int64_t whole = g.x_bf16 ? 8 : 4;
-        g.x_vec = c.p->n % whole == 0 && c.p->ld_x % whole == 0;
-        product<ns::EPI_FINAL>(c, g, a, b, nullptr, *table);
-    }
-}
-
-void run_batch(const orthdion_muon_plan* p, const ns::Table& t, bool update, char* scratch, cudaStream_t st) {
-    const Scratch sc = scratch_layout(p, t.count);
-    const int terms = terms_of(p);
-    ns::PrepArgs a{};
-    a.rows = p->m; a.cols = p->n; a.ld_g = p->ld_g; a.ld_m = p->ld_m;
-    a.g_bf16 = p->g_dtype == ORTHDION_DTYPE_BF16; a.nesterov = p->nesterov;
-    a.mu = (float)p->mu; a.rest = (float)(1.0 - p->mu);
-    a.eps = p->eps;
-    a.terms = terms;
-    a.vec = p->n % 8 == 0 && p->ld_g % 8 == 0 && (!update || p->ld_m % 4 == 0);
-    a.part = reinterpret_cast<double*>(scratch + sc.part);
-    a.slot = reinterpret_cast<ns::Slot*>(scratch + sc.slot);
-    a.img = reinterpret_cast<__half*>(scratch + sc.x[0]);
-    a.pitch = sc.x_pitch; a.term_stride = sc.x_term; a.mat_stride = sc.x_mat;
-    // four chunks of 8 a thread, and no more blocks than eight per multiprocessor
-    const int64_t chunks = (p->n + 7) / 8 * p->m;
-    const int64_t most = std::max<int64_t>(1, 8 * sm_count() / t.count);
-    a.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({(chunks + 1023) / 1024, most, ns::MAX_PARTS}));
-    launch(ns::norm_kernel, dim3((unsigned)a.parts, (unsigned)t.count), 256, 0, 1, prof::S_NS_BUFFER, st, t, a);
-    const unsigned blocks = (unsigned)std::max<int64_t>(1, std::min<int64_t>((chunks + 1023) / 1024, most));
-    launch(ns::prep_kernel, dim3(blocks, (unsigned)t.count), 256, 0, 1, prof::S_NS_BUFFER, st, t, a);
-
-    const Chain c{p, t.count, terms, a.slot, st};
-    const int64_t s = std::min(p->m, p->n);
-    Image x[2], sq[4];
-    for (int i = 0; i < 2; ++i) x[i] = Image{scratch + sc.x[i], p->m, p->n, sc.x_pitch, sc.x_term, sc.x_mat};
-    for (int i = 0; i < 4; ++i) sq[i] = Image{scratch + sc.sq[i], s, s, sc.s_pitch, sc.s_term, sc.s_mat};
-    const std::vector<int> groups = group_steps(p);
-    const float unit = 1.f / ns::UNIT;
-    int step = 0, cur = 0;
-    auto poly = [&](const Image& out) {          // Q = a I + b A + c A^2 of the next step, A in sq[0]
-        const float* k = p->abc[step++];
-        square_product(c, sq[0], sq[0], out, k[2] * unit, &sq[0], k[1], k[0] * ns::UNIT);
-    };
-    for (size_t gi = 0; gi < groups.size(); ++gi) {
-        const bool first = gi == 0, last = gi + 1 == groups.size();
-        gram_product(c, x[cur], sq[0], first);
-        poly(sq[1]);
-        if (groups[gi] == 2) {
-            square_product(c, sq[1], sq[0], sq[2], unit);       // A' = Q (Q A)
-            square_product(c, sq[1], sq[2], sq[0], unit);
-            poly(sq[3]);
-            square_product(c, sq[3], sq[1], sq[2], unit);       // P = Q' Q
+    if (!enc) { engine_error() = 1; return; }
+    const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
+    auto map = [&](CUtensorMap* out, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+        const CUresult r = enc(out, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+        if (r != CUDA_SUCCESS) {
+            std::fprintf(stderr, "orthdion: cuTensorMapEncodeTiled failed (%d)\n", (int)r);
+            engine_error() = 2;
         }
-        apply_product(c, sq[groups[gi] == 2 ? 2 : 1], x[cur], last ? nullptr : &x[1 - cur], first, &t, update);
-        cur = 1 - cur;
+    };
+    const cuuint64_t kd[4] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)terms, (cuuint64_t)count};
+    const cuuint64_t ks[3] = {(cuuint64_t)pitch * 2, (cuuint64_t)term * 2, (cuuint64_t)mat * 2};
+    const cuuint32_t kb[4] = {64, 128, (cuuint32_t)terms, 1};
+    map(k, 4, kd, ks, kb);
+    const cuuint64_t md[5] = {64, (cuuint64_t)rows, (cuuint64_t)pitch / 64, (cuuint64_t)terms, (cuuint64_t)count};
+    const cuuint64_t ms[4] = {(cuuint64_t)pitch * 2, 128, (cuuint64_t)term * 2, (cuuint64_t)mat * 2};
+    const cuuint32_t mb[5] = {64, 64, 2, (cuuint32_t)terms, 1};
+    map(mn, 5, md, ms, mb);
+}
+
+int g_pairs[kMaxDevices] = {};       // CTA pairs of the chain kernel that the device runs at once; written under ensure_attributes()'s lock
+
+int current_device() {
+    int dev = -1;
+    return cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < kMaxDevices ? dev : -1;
+}
+
+// One launch: the buffers' norms and images class by class, then all products.
+void run_launch(const orthdion_muon_t* hs, const Launch& l, void* const* X, float* const* M, const void* const* G, bool update, char* ws,
+                char* scratch, cudaStream_t st) {
+    std::unique_ptr<ns::ChainArgs> args(new ns::ChainArgs());
+    ns::Table all{};
+    const int terms = terms_of(hs[l.classes[0][0]]), pairs = g_pairs[current_device()];
+    args->classes = (int32_t)l.classes.size();
+    for (size_t k = 0; k < l.classes.size(); ++k) {
+        const std::vector<int>& idx = l.classes[k];
+        const orthdion_muon_plan* p = hs[idx[0]];
+        const Scratch sc = scratch_layout(p, (int)idx.size());
+        char* base = scratch + l.off[k];
+        ns::Class& c = args->c[k];
+        ns::Table t{};
+        t.count = c.count = (int32_t)idx.size();
+        c.first = all.count;
+        for (int i = 0; i < t.count; ++i) {
+            const int j = idx[i];
+            t.w[i] = all.w[all.count++] = ns::Mat{G[j], update ? M[j] : nullptr, X[j], reinterpret_cast<int32_t*>(ws) + j};
+        }
+        c.m = (int32_t)p->m; c.n = (int32_t)p->n;
+        c.steps = p->steps;
+        const Groups g = group_steps(p);
+        c.pair_first = g.pair_first; c.pair_last = g.pair_last;
+        std::memcpy(c.abc, p->abc, sizeof(c.abc));
+        c.slot = reinterpret_cast<ns::Slot*>(base + sc.slot);
+        c.x_pitch = sc.x_pitch; c.x_term = sc.x_term; c.x_mat = sc.x_mat;
+        c.s_pitch = sc.s_pitch; c.s_term = sc.s_term; c.s_mat = sc.s_mat;
+        const int64_t s = std::min(p->m, p->n);
+        for (int i = 0; i < 2; ++i) {
+            c.x[i] = reinterpret_cast<__half*>(base + sc.x[i]);
+            encode(&c.k_x[i], &c.mn_x[i], c.x[i], p->n, p->m, terms, c.count, sc.x_pitch, sc.x_term, sc.x_mat);
+        }
+        for (int i = 0; i < 4; ++i) {
+            c.sq[i] = reinterpret_cast<__half*>(base + sc.sq[i]);
+            encode(&c.k_sq[i], &c.mn_sq[i], c.sq[i], s, s, terms, c.count, sc.s_pitch, sc.s_term, sc.s_mat);
+        }
+        c.tiles_sq = sc.tiles_sq; c.tiles_x = sc.tiles_x; c.counts = sc.counts;
+        c.tile_done = reinterpret_cast<uint32_t*>(base + sc.tile_done);
+        c.update = update;
+        c.x_bf16 = p->x_dtype == ORTHDION_DTYPE_BF16;
+        c.ld_x = p->ld_x;
+        const int64_t whole = c.x_bf16 ? 8 : 4;
+        c.x_vec = p->n % whole == 0 && p->ld_x % whole == 0;
+        c.wc = 1.f - p->eta * p->wd; c.wd = p->eta * p->scale;
+        args->stages = std::max(args->stages, ns::products(c.steps, c.pair_first, c.pair_last));
+
+        ns::PrepArgs a{};
+        a.rows = p->m; a.cols = p->n; a.ld_g = p->ld_g; a.ld_m = p->ld_m;
+        a.g_bf16 = p->g_dtype == ORTHDION_DTYPE_BF16; a.nesterov = p->nesterov;
+        a.mu = (float)p->mu; a.rest = (float)(1.0 - p->mu);
+        a.eps = p->eps;
+        a.terms = terms;
+        a.vec = p->n % 8 == 0 && p->ld_g % 8 == 0 && (!update || p->ld_m % 4 == 0);
+        a.part = reinterpret_cast<double*>(base + sc.part);
+        a.slot = c.slot;
+        a.counts = c.tile_done; a.counts_n = c.counts;
+        a.img = c.x[0];
+        a.pitch = sc.x_pitch; a.term_stride = sc.x_term; a.mat_stride = sc.x_mat;
+        // four chunks of 8 a thread, and no more blocks than eight per multiprocessor
+        const int64_t chunks = (p->n + 7) / 8 * p->m, most = std::max<int64_t>(1, 8 * sm_count() / t.count);
+        a.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({(chunks + 1023) / 1024, most, ns::MAX_PARTS}));
+        launch(ns::norm_kernel, dim3((unsigned)a.parts, (unsigned)t.count), 256, 0, 1, prof::S_NS_BUFFER, st, t, a);
+        const unsigned blocks = (unsigned)std::max<int64_t>(1, std::min<int64_t>((chunks + 1023) / 1024, most));
+        launch(ns::prep_kernel, dim3(blocks, (unsigned)t.count), 256, 0, 1, prof::S_NS_BUFFER, st, t, a);
     }
+    if (engine_error()) return;
+
+    int units = 0;                 // of the products with the most tiles
+    for (int k = 0; k < args->classes; ++k) units += std::max(args->c[k].tiles_sq, args->c[k].tiles_x) * args->c[k].count;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(2 * std::min(pairs, units)));
+    cfg.blockDim = dim3(ns::THREADS);
+    cfg.dynamicSmemBytes = ns::SMEM_BYTES;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    // (pairs wait for one another's tiles: all of them run at once, or none)
+    attr[1].id = cudaLaunchAttributeCooperative;
+    attr[1].val.cooperative = 1;
+    cfg.attrs = attr; cfg.numAttrs = 2;
+    prof::Scope scope(prof::S_NS_PRODUCT, st);
+    const cudaError_t e = terms == 2 ? cudaLaunchKernelEx(&cfg, ns::chain_kernel<2>, all, *args) : cudaLaunchKernelEx(&cfg, ns::chain_kernel<1>, all, *args);
+    if (e != cudaSuccess) engine_error() = LAUNCH_FAILED;
 }
 
 int ensure_attributes() {
     static std::mutex mu;
     static signed char state[kMaxDevices] = {};   // 0 unknown, 1 ok, -1 failed
-    int dev = -1;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return ORTHDION_ERR_CUDA;
+    const int dev = current_device();
+    if (dev < 0) return ORTHDION_ERR_CUDA;
     std::lock_guard<std::mutex> lock(mu);
     if (state[dev]) return state[dev] > 0 ? 0 : ORTHDION_ERR_CUDA;
     cudaError_t e = cudaSuccess;
     auto set = [&](auto* kernel) {
         if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ns::SMEM_BYTES);
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3((unsigned)(sm_count() / 2 * 2)); cfg.blockDim = dim3(ns::THREADS);
+        cfg.dynamicSmemBytes = ns::SMEM_BYTES;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr; cfg.numAttrs = 1;
+        int n = 0;
+        if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+        if (e == cudaSuccess && n < 1) e = cudaErrorInvalidConfiguration;
+        g_pairs[dev] = g_pairs[dev] ? std::min(g_pairs[dev], n) : n;
     };
-#define OD_SET(...) set(ns::gemm_kernel<__VA_ARGS__, ns::EPI_IMAGE, ns::NoTable>); set(ns::gemm_kernel<__VA_ARGS__, ns::EPI_FINAL, ns::Table>);
-    OD_SET(true, 256, 1)
-    OD_SET(true, 256, 2)
-    OD_SET(false, 128, 1)
-    OD_SET(false, 128, 2)
-#undef OD_SET
+    set(ns::chain_kernel<1>);
+    set(ns::chain_kernel<2>);
     if (e != cudaSuccess) std::fprintf(stderr, "orthdion: kernel attribute setup failed on device %d: %s\n", dev, cudaGetErrorString(e));
     state[dev] = e == cudaSuccess ? 1 : -1;
     return e == cudaSuccess ? 0 : ORTHDION_ERR_CUDA;
@@ -382,38 +346,17 @@ int run_call(const orthdion_muon_t* hs, int32_t count, void* const* X, float* co
     }
     if (twice(X, count) || (update && twice(reinterpret_cast<const void* const*>(M), count))) return ORTHDION_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(workspace) % 256) return ORTHDION_ERR_WORKSPACE;
-    const Batching bt = make_batches(hs, count);
-    if (workspace_bytes < status_bytes(count) + bt.scratch) return ORTHDION_ERR_WORKSPACE;
+    size_t scratch = 0;
+    const std::vector<Launch> launches = make_launches(hs, count, &scratch);
+    if (workspace_bytes < status_bytes(count) + scratch) return ORTHDION_ERR_WORKSPACE;
     int e = ensure_attributes();
     if (e) return e;
     char* ws = reinterpret_cast<char*>(workspace);
-    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    const int lanes = std::min(bt.lanes, g_lanes.load());
-    DeviceLanes* dl = lanes > 1 ? device_lanes() : nullptr;
-    std::unique_lock<std::mutex> lock;
-    if (dl) {
-        lock = std::unique_lock<std::mutex>(dl->mu);
-        cudaEventRecord(dl->fork, st);
-        for (int l = 0; l < lanes; ++l) cudaStreamWaitEvent(dl->lane[l], dl->fork, 0);
-    }
     engine_error() = 0;
-    overlap_launches() = dl == nullptr;      // (CTAs that wait for one chain's next launch would keep the others' off the multiprocessors)
-    for (size_t b = 0; b < bt.batches.size() && !engine_error(); ++b) {
-        const auto& idx = bt.batches[b];
-        ns::Table t{};
-        t.count = (int32_t)idx.size();
-        for (int k = 0; k < t.count; ++k) {
-            const int i = idx[k];
-            t.w[k] = ns::Mat{G[i], update ? M[i] : nullptr, X[i], reinterpret_cast<int32_t*>(ws) + i};
-        }
-        // (lane b % bt.lanes, whose scratch this is, is wholly on one stream)
-        run_batch(hs[idx[0]], t, update, ws + status_bytes(count) + bt.off[b], dl ? dl->lane[(b % bt.lanes) % lanes] : st);
-    }
-    if (dl) {
-        for (int l = 0; l < lanes; ++l) {
-            cudaEventRecord(dl->done[l], dl->lane[l]);
-            cudaStreamWaitEvent(st, dl->done[l], 0);
-        }
+    overlap_launches() = true;
+    for (const Launch& l : launches) {
+        run_launch(hs, l, X, M, G, update, ws, ws + status_bytes(count), reinterpret_cast<cudaStream_t>(stream));
+        if (engine_error()) break;
     }
     return launch_outcome();
 }
@@ -586,7 +529,9 @@ size_t orthdion_muon_workspace_bytes_grouped(const orthdion_muon_t* hs, int32_t 
     for (int i = 0; i < count; ++i)
         if (!valid(hs[i])) return 0;
     return guarded((size_t)0, [&] {
-        return status_bytes(count) + make_batches(hs, count).scratch;
+        size_t scratch = 0;
+        make_launches(hs, count, &scratch);
+        return status_bytes(count) + scratch;
     });
 }
 

@@ -43,7 +43,8 @@ struct Table {
 struct Slot {
     float sigma;       // UNIT / (stored |X0| + stored eps): how much larger the normalised matrix is than the stored one
     int32_t status;
-    int32_t pad[2];
+    uint32_t done;     // epilogue warps that have finished a tile of one of its products
+    int32_t pad;
 };
 
 // ---- the buffer B, its norm, its image ---------------------------------------------------------
@@ -56,6 +57,8 @@ struct PrepArgs {
     int32_t vec;                 // rows start on 16-byte boundaries
     double* part;                // [matrix][MAX_PARTS]
     Slot* slot;
+    uint32_t* counts;            // [matrix][counts_n], cleared
+    int32_t counts_n;
     __half* img;
     int64_t pitch, term_stride, mat_stride;      // of the image, in elements
 };
@@ -194,6 +197,7 @@ __global__ void __launch_bounds__(256) prep_kernel(const __grid_constant__ Table
         a.slot[blockIdx.y] = s;
         *w.status = s.status;
     }
+    for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < a.counts_n; i += gridDim.x * blockDim.x) a.counts[(int64_t)blockIdx.y * a.counts_n + i] = 0;
     if (!finite) return;
     __half* img = a.img + (int64_t)blockIdx.y * a.mat_stride;
     auto write = [&](const Raw& r, int64_t row, int64_t col) {
@@ -229,34 +233,151 @@ __global__ void __launch_bounds__(256) prep_kernel(const __grid_constant__ Table
     else for_chunks<2, false>(w, a, blockIdx.x, gridDim.x, write);
 }
 
-// ---- products between images ---------------------------------------------------------------------
-// D = alpha sigma^p (A B^T) + beta C + diag I, with A rows x depth, B cols x depth.
-enum Epi : int { EPI_IMAGE = 0, EPI_FINAL = 1 };
-
-constexpr int STAGE_BYTES = 196608;           // operand ring
+// ---- the products: one persistent kernel for all steps of a batch ------------------------------------
+// A matrix goes through its products one after the other:
+//   group of one step    A = X X^T;  Q = a I + b A + c A^2;  X' = Q X
+//   group of two steps   A = X X^T;  Q = a I + b A + c A^2;  T = Q A;  A' = Q T;  Q' = a' I + b' A' + c' A'^2;  P = Q' Q;  X' = P X
+// (X in turns in two images; sq[0]: A and Q', sq[1]: Q, sq[2]: T and P, sq[3]: A').  The 256 x 256 tiles of one product of one matrix are
+// units of work; CTA pairs take the units of all matrices in turn, product after product.
+//
+// Symmetric results.  All but X are polynomials of one symmetric matrix: tiles on and below the diagonal are computed and stored, and an operand
+// tile above it is read from its mirror image, along columns in place of rows (the MMA takes either).
+//
+// Order.  A unit loads a tile of an operand once its count has come to what the product that writes it leaves there, so the first units
+// of a product run beside the last ones of the product before.  A unit of product k stores its result when all units of product k - 2 are
+// done; no product writes what the one before reads.  Every unit waits for units in front of it only, and all pairs run at once.
+// (One launch per product: 10 of 60 us of each between the last MMA of one and the first of the next for a 4096 x 4096 matrix, 6 of 10 for
+// 768 x 2048, and multiprocessors without work at the end of each.  One kernel that waits for whole products: 15 of 80 us, the results'
+// stores and their fences among them.)
+constexpr int STAGE_RING = 196608;            // bytes of the operand ring
 constexpr int THREADS = 32 * 10;              // producer, issuer, eight epilogue warps
-constexpr int MAX_STAGES = 8;
+constexpr int MAX_STAGES = 6;
+constexpr int SMEM_BYTES = 1024 + STAGE_RING + 8 * 4096 + 256;
+constexpr int TM = 256;                       // rows (128 of each CTA of a pair) and columns of a tile
+constexpr int NC = TM / 2;                    // columns of an epilogue warp
 constexpr int GROUP_ROWS = 8;                 // tile rows that are walked together, column by column
+constexpr int ARRIVALS = 16;                  // at a count for one unit: the epilogue warps of a pair
+constexpr int MAX_CLASSES = 8;
+constexpr int MAX_ITER = 32;                  // steps of a schedule
 
-struct GemmArgs {
-    int32_t rows, cols, kblocks, chunk;       // chunk: depth blocks that are summed in tensor memory
-    int32_t m_tiles, n_tiles, tiles, total;   // tiles: of one matrix
-    int32_t sym;                              // symmetric result: tiles on and below the diagonal, mirrored
-    int32_t a_mn, b_mn;                       // 1: depth runs along the rows of the image
-    int32_t sigma_pow;
-    float alpha, beta, diag;
-    __half* out;                              // image of the result ...
-    const __half* add;                        // ... and of C, laid out alike; null: D = alpha sigma^p (A B^T)
-    int64_t pitch, term_stride, mat_stride;
+// Matrices of one plan.
+struct Class {
+    // Boxes over an image, all planes of one matrix: 64 columns of 128 rows, an operand tile along rows (K-major); and two groups of
+    // 64 columns of 64 rows, one along columns (MN-major; what lies between the last column and the pitch only reaches results beyond the edge).
+    alignas(64) CUtensorMap k_x[2];
+    CUtensorMap k_sq[4], mn_x[2], mn_sq[4];
+    __half* x[2];
+    __half* sq[4];
+    int64_t x_pitch, x_term, x_mat, s_pitch, s_term, s_mat;     // in elements
     Slot* slot;
-    int32_t count;
-    int32_t update, x_bf16, x_vec;            // EPI_FINAL: X <- wc X - wd D, or X <- D; x_vec: rows of X on 16-byte boundaries, and whole vectors
-    float wc, wd;
+    uint32_t* tile_done;                      // counts of the tiles of sq[0] to sq[3] (row by row below the diagonal) and of X
     int64_t ld_x;
-    alignas(64) CUtensorMap map_a;
-    alignas(64) CUtensorMap map_b;
+    int32_t m, n, count, first;               // first: its first matrix in the table
+    int32_t steps, pair_first, pair_last;     // steps of the iteration; whether the first and the last two of them are one group
+    int32_t tiles_sq, tiles_x, counts;        // tiles of one s x s product, of one product with X; counts of one matrix
+    int32_t update, x_bf16, x_vec;
+    float wc, wd;
+    float abc[MAX_ITER][3];
 };
-struct NoTable { int32_t unused; };
+__host__ __device__ constexpr int tiles_along(int n) { return (n + TM - 1) / TM; }
+struct ChainArgs {
+    int32_t classes, stages;                  // stages: most products of a class
+    Class c[MAX_CLASSES];
+};
+
+enum OpKind : int { OP_GRAM, OP_POLY, OP_MUL, OP_APPLY };
+// One product of a class.
+struct Op {
+    int kind, group, step;                    // step: whose coefficients OP_POLY takes
+    int a, b, out;                            // images: 0 to 3 sq, 4 and 5 X; out < 0: the caller's matrix
+    bool last, second;                        // of the last group; behind A' of a group of two
+};
+__host__ __device__ inline int products(int steps, int pair_first, int pair_last) { return 3 * steps + (pair_first ? 1 : 0) + (pair_last ? 1 : 0); }
+__device__ __forceinline__ Op op_of(const Class& c, int stage) {
+    Op o;
+    const int p0 = c.pair_first ? 7 : 0, singles = c.steps - 2 * c.pair_first - 2 * c.pair_last;
+    int j, first_step;
+    bool pair;
+    if (stage < p0) {
+        o.group = 0; j = stage; pair = true; first_step = 0;
+    } else if (stage < p0 + 3 * singles) {
+        const int k = (stage - p0) / 3;
+        o.group = c.pair_first + k; j = stage - p0 - 3 * k; pair = false; first_step = 2 * c.pair_first + k;
+    } else {
+        o.group = c.pair_first + singles; j = stage - p0 - 3 * singles; pair = true; first_step = c.steps - 2;
+    }
+    const int x = 4 + (o.group & 1), nx = 4 + (~o.group & 1);
+    o.last = first_step + (pair ? 2 : 1) == c.steps;
+    o.step = first_step;
+    const int end = pair ? 6 : 2;
+    if (j == 0) { o.kind = OP_GRAM; o.a = o.b = x; o.out = 0; }
+    else if (j == end) { o.kind = OP_APPLY; o.a = pair ? 2 : 1; o.b = x; o.out = o.last ? -1 : nx; }
+    else if (j == 1) { o.kind = OP_POLY; o.a = o.b = 0; o.out = 1; }
+    else if (j == 2) { o.kind = OP_MUL; o.a = 1; o.b = 0; o.out = 2; }
+    else if (j == 3) { o.kind = OP_MUL; o.a = 1; o.b = 2; o.out = 3; }
+    else if (j == 4) { o.kind = OP_POLY; o.a = o.b = 3; o.out = 0; o.step = first_step + 1; }
+    else { o.kind = OP_MUL; o.a = 0; o.b = 1; o.out = 2; }
+    o.second = pair && j >= 4;
+    return o;
+}
+// How often the tiles of an image have been written when this product of its group reads it.
+__device__ __forceinline__ uint32_t writes_of(const Class& c, const Op& o, int image) {
+    const int pairs = c.pair_first && o.group > 0 ? 1 : 0;             // groups of two in front of this one
+    switch (image) {
+        case 0: return o.group + pairs + (o.second ? 2 : 1);
+        case 1: return o.group + 1;
+        case 2: return 2 * pairs + (o.kind == OP_APPLY ? 2 : 1);
+        case 3: return pairs + 1;
+        default: return (o.group + 1) / 2;                              // X: by the product with X of the group before
+    }
+}
+
+// A walk over the units of a launch, one pair's share.
+struct Walk {
+    int stage, cls, base;      // the (product, class) that `unit` is in, and its first unit
+    int unit;
+};
+struct Unit {
+    int cls, mat, stage;
+    int ti, tj, rows, cols, kblocks;          // tile row and column
+    Op op;
+};
+// Makes w.unit a unit of (w.stage, w.cls), or returns false behind the last.
+__device__ __forceinline__ bool find_unit(const ChainArgs& g, Walk& w, Unit& u) {
+    while (true) {
+        if (w.stage >= g.stages) return false;
+        const Class& c = g.c[w.cls];
+        int units = 0;
+        if (w.stage < products(c.steps, c.pair_first, c.pair_last)) {
+            u.op = op_of(c, w.stage);
+            units = (u.op.kind == OP_APPLY ? c.tiles_x : c.tiles_sq) * c.count;
+        }
+        if (w.unit < w.base + units) break;
+        w.base += units;
+        if (++w.cls == g.classes) { w.cls = 0; ++w.stage; }
+    }
+    const Class& c = g.c[w.cls];
+    const bool apply = u.op.kind == OP_APPLY;
+    const int s = min(c.m, c.n), l = max(c.m, c.n), tiles = apply ? c.tiles_x : c.tiles_sq;
+    int t = w.unit - w.base;
+    u.cls = w.cls; u.stage = w.stage;
+    u.mat = t / tiles;
+    t -= u.mat * tiles;
+    u.rows = apply ? c.m : s; u.cols = apply ? c.n : s;
+    u.kblocks = ((u.op.kind == OP_GRAM ? l : s) + 63) / 64;
+    if (!apply) {
+        u.ti = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
+        while (u.ti * (u.ti + 1) / 2 > t) --u.ti;
+        while ((u.ti + 1) * (u.ti + 2) / 2 <= t) ++u.ti;
+        u.tj = t - u.ti * (u.ti + 1) / 2;
+    } else {
+        const int n_tiles = tiles_along(u.cols), m_tiles = tiles_along(u.rows);
+        const int per = GROUP_ROWS * n_tiles, grp = t / per, first = grp * GROUP_ROWS, high = min(GROUP_ROWS, m_tiles - first), in = t - grp * per;
+        u.tj = in / high;
+        u.ti = first + in - u.tj * high;
+    }
+    return true;
+}
 
 __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
@@ -265,17 +386,18 @@ template <class T> __device__ __forceinline__ T from_float(float v) {
     else return v;
 }
 
-__device__ __forceinline__ void tma_load4(uint32_t dst, const CUtensorMap* map, int x, int row, int term, int mat, uint32_t bar, bool pair) {
-    if (pair)
-        asm volatile(
-            "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
-            ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(row), "r"(term), "r"(mat), "r"(bar) : "memory");
-    else
-        asm volatile(
-            "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
-            ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(row), "r"(term), "r"(mat), "r"(bar) : "memory");
+// The box of a map at (column, row) or (row, 64-column group) of one matrix, for a CTA of a pair: counted on the leader's mbarrier.
+__device__ __forceinline__ void tma_load_k(uint32_t dst, const CUtensorMap* map, int col, int row, int mat, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(col), "r"(row), "r"(0), "r"(mat), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&v)[32]) {
+__device__ __forceinline__ void tma_load_mn(uint32_t dst, const CUtensorMap* map, int row, int group, int mat, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(group), "r"(0), "r"(mat), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* v) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
         "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
@@ -293,139 +415,165 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const float* v) {
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// Rows of a result tile, and rows of B that one CTA holds of it.
-template <bool PAIR> __host__ __device__ constexpr int tile_rows() { return PAIR ? 256 : 128; }
-template <bool PAIR, int BN> __host__ __device__ constexpr int side_rows() { return PAIR ? BN / 2 : BN; }
-template <bool PAIR, int BN, int TERMS> __host__ __device__ constexpr int stage_bytes() { return (128 + side_rows<PAIR, BN>()) * 128 * TERMS; }
-template <bool PAIR, int BN, int TERMS> __host__ __device__ constexpr int stages() {
-    constexpr int n = STAGE_BYTES / stage_bytes<PAIR, BN, TERMS>();
-    return n < MAX_STAGES ? n : MAX_STAGES;
-}
-constexpr int SMEM_BYTES = 1024 + STAGE_BYTES + 8 * 4096 + 256;
-
-struct Tile { int mat, row0, col0; bool active, mirror; };
-
-template <bool PAIR, int BN>
-__device__ __forceinline__ Tile decode(const GemmArgs& g, int t) {
-    constexpr int TM = tile_rows<PAIR>();
-    Tile r;
-    r.mat = t / g.tiles;
-    t -= r.mat * g.tiles;
-    int i, j;
-    if (g.sym) {
-        // tiles before tile row i: i (i + 1) / 2 of square tiles, i (i + 1) of tiles half as wide as high
-        constexpr int Q = TM / BN;
-        i = Q == 1 ? (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f) : (int)((sqrtf(4.f * t + 1.f) - 1.f) * 0.5f);
-        auto before = [](int k) { return Q == 1 ? k * (k + 1) / 2 : k * (k + 1); };
-        while (before(i) > t) --i;
-        while (before(i + 1) <= t) ++i;
-        j = t - before(i);
-    } else {
-        const int per = GROUP_ROWS * g.n_tiles, grp = t / per;
-        const int first = grp * GROUP_ROWS, high = min(GROUP_ROWS, g.m_tiles - first);
-        const int in = t - grp * per;
-        j = in / high;
-        i = first + in - j * high;
+// One side of a product: an image, read along the unit's rows (or columns) `tile`.
+struct Side {
+    int image, tile;
+    bool sym;              // a symmetric image: mirrored above the diagonal
+    bool mn;               // X along its columns: depth runs down its rows
+    __device__ __forceinline__ bool along_columns(int kb) const { return sym ? kb / 4 > tile : mn; }
+    // index of the tile of depth block kb in its image's counts
+    __device__ __forceinline__ int place(const Class& c, int kb) const {
+        const int k = kb / 4;
+        if (sym) {
+            const int hi = max(k, tile), lo = min(k, tile);
+            return image * c.tiles_sq + hi * (hi + 1) / 2 + lo;
+        }
+        const int row = mn ? k : tile, col = mn ? tile : k;
+        return 4 * c.tiles_sq + (image - 4) * c.tiles_x + row * tiles_along(c.n) + col;
     }
-    r.row0 = i * TM; r.col0 = j * BN;
-    r.active = r.col0 < g.cols;
-    r.mirror = g.sym && r.col0 + BN <= r.row0;
-    return r;
+};
+__device__ __forceinline__ void sides_of(const Class& c, const Unit& u, Side& a, Side& b) {
+    const bool wide = c.m <= c.n, gram_tall = u.op.kind == OP_GRAM && !wide;
+    a = Side{u.op.a, u.ti, u.op.a < 4, gram_tall};
+    b = Side{u.op.b, u.tj, u.op.b < 4, gram_tall || (u.op.kind == OP_APPLY && wide)};
+    // X is the second side of a product with a wide matrix, the first with a tall one
+    if (u.op.kind == OP_APPLY && !wide) {
+        a = Side{u.op.b, u.ti, false, false};
+        b = Side{u.op.a, u.tj, true, false};
+    }
 }
 
-// The rows of one warp (row_w + lane) and NC columns from col_w of a result in tensor memory at d -> image, 32 columns at a time,
-// through shared memory so that four lanes write 64 bytes of a row; with `mirror` also to the mirrored place, where pairs of rows and
-// columns are exchanged between neighbouring lanes first.  (With TMA stores out of two such blocks in turn a block took 1200 cycles,
-// most of them the wait until the one before was read, and its mirror image in 4-byte stores as long again.)
-template <int TERMS, int NC>
-__device__ __forceinline__ void image_epilogue(const GemmArgs& g, uint32_t d, float alpha, int mat, int row_w, int lane, int col_w, bool mirror,
-                                               unsigned char* stage_ptr) {
-    const int row = row_w + lane;
-    const int64_t base = mat * g.mat_stride;
-    const __half* add = g.add ? g.add + base + (int64_t)min(row, g.rows - 1) * g.pitch : nullptr;
-    const int sr = lane / 4, sc = lane % 4;              // row and 16-byte chunk that this lane moves out
-    const bool odd = lane & 1;
-    unsigned char* mir_ptr = stage_ptr + 2048;
-    uint4 cq[TERMS][4];
-    auto fetch = [&](int col) {
+__device__ __forceinline__ uint32_t load_acquire(const uint32_t* p) {
+    uint32_t v;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+// Waits until a count has come to `want`; then what was written before it was raised can be read.
+__device__ __forceinline__ bool wait_count(const uint32_t* p, uint32_t want, volatile int* abort_flag) {
+    if ((int32_t)(load_acquire(p) - want) >= 0) return true;
+    const long long t0 = clock64();
+    for (int spins = 0;; ++spins) {
+        if ((int32_t)(load_acquire(p) - want) >= 0) return true;
+        if ((spins & 15) == 15) {
+            if (*abort_flag) return false;
+            if (clock64() - t0 > WAIT_LIMIT_CYCLES) { *abort_flag = 1; return false; }
+        }
+        __nanosleep(20);
+    }
+}
+// Units of a matrix's products before product `stage`, which begins group `group` or belongs to it.
+__device__ __forceinline__ uint32_t units_before(const Class& c, int stage, int group) {
+    return (uint32_t)((stage - group) * c.tiles_sq + group * c.tiles_x);
+}
+
+// The rows of one warp (row_w + lane) and NC columns from col_w of a result in tensor memory at d -> image, through 4 KB of shared memory:
+// 64 columns of one plane or 32 of two, with as many lanes to a row as its bytes fill; C comes the same way and is replaced in place.
+// (With C read by each lane along its own row, 32 lines a load, a tile took 3.5 us longer.)
+struct Out {
+    __half* img;                 // image of the result ...
+    const __half* add;           // ... and of C, laid out alike (null: none): alpha D + beta C + diag I
+    int64_t pitch, term;
+    int rows, cols;
+    float beta, diag;
+};
+template <int TERMS>
+__device__ __forceinline__ void image_epilogue(const Out& g, uint32_t d, float alpha, int row_w, int lane, int col_w, unsigned char* stage_ptr) {
+    constexpr int W = 64 / TERMS, CH = W / 8, RPI = 32 / CH, IT = 32 / RPI;      // chunks of 16 bytes a row, rows a turn, turns
+    const int sr = lane / CH, sc = lane % CH;                // (sr, sc): row and chunk that this lane moves
+    auto at = [](int t, int r, int ch) { return t * 2048 + r * (2 * W) + ((CH == 8 ? ch ^ (r & 7) : ch ^ ((r >> 1) & 3)) << 4); };
+    const int64_t lane_at = (int64_t)(row_w + sr) * g.pitch + col_w + sc * 8;
+    uint4 cq[TERMS][IT];
+    auto fetch = [&](int q) {
 #pragma unroll
         for (int t = 0; t < TERMS; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) cq[t][i] = *reinterpret_cast<const uint4*>(add + t * g.term_stride + col + i * 8);
+            for (int i = 0; i < IT; ++i)
+                if (row_w + sr + RPI * i < g.rows)               // (L1 may hold what the image was before)
+                    cq[t][i] = __ldcg(reinterpret_cast<const uint4*>(g.add + t * g.term + lane_at + RPI * i * g.pitch + q * W));
     };
-    if (add) fetch(col_w);
+    if (g.add) fetch(0);
 #pragma unroll 1
-    for (int q = 0; q < NC / 32; ++q) {
-        const int col = col_w + q * 32;
+    for (int q = 0; q < NC / W; ++q) {
+        const int col = col_w + q * W;
         if (col >= g.cols) break;
-        float v[32];
-        {
-            uint32_t u[32];
-            tmem_ld32(d + q * 32, u);
-            tmem_ld_wait();
+        if (g.add) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) v[e] = alpha * __uint_as_float(u[e]);
+            for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+                for (int i = 0; i < IT; ++i) *reinterpret_cast<uint4*>(stage_ptr + at(t, sr + RPI * i, sc)) = cq[t][i];
+            if (q + 1 < NC / W && col + W < g.cols) fetch(q + 1);
+            __syncwarp();
         }
-        if (add) {
+#pragma unroll
+        for (int h = 0; h < W / 32; ++h) {
+            float v[32];
+            {
+                uint32_t u[32];
+                tmem_ld32(d + q * W + h * 32, u);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) v[e] = alpha * __uint_as_float(u[e]);
+            }
+            if (g.add) {
+#pragma unroll
+                for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint4 x = *reinterpret_cast<const uint4*>(stage_ptr + at(t, lane, h * 4 + i));
+                        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
+                            v[i * 8 + 2 * k] = fmaf(g.beta, f.x, v[i * 8 + 2 * k]);
+                            v[i * 8 + 2 * k + 1] = fmaf(g.beta, f.y, v[i * 8 + 2 * k + 1]);
+                        }
+                    }
+                if (col + h * 32 == row_w) {          // the block on the diagonal
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[e] += e == lane ? g.diag : 0.f;
+                }
+            }
 #pragma unroll
             for (int t = 0; t < TERMS; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint32_t h[4] = {cq[t][i].x, cq[t][i].y, cq[t][i].z, cq[t][i].w};
+                    uint32_t w[4];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[k]));
-                        v[i * 8 + 2 * k] = fmaf(g.beta, f.x, v[i * 8 + 2 * k]);
-                        v[i * 8 + 2 * k + 1] = fmaf(g.beta, f.y, v[i * 8 + 2 * k + 1]);
+                        float &x = v[i * 8 + 2 * k], &y = v[i * 8 + 2 * k + 1];
+                        w[k] = pack_f16x2(x, y);
+                        if (TERMS == 2 && t == 0) {
+                            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
+                            x -= f.x; y -= f.y;
+                        }
                     }
+                    *reinterpret_cast<uint4*>(stage_ptr + at(t, lane, h * 4 + i)) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
-            if (col == row_w) {          // the block on the diagonal
-#pragma unroll
-                for (int e = 0; e < 32; ++e) v[e] += e == lane ? g.diag : 0.f;
-            }
-            if (q + 1 < NC / 32 && col + 32 < g.cols) fetch(col + 32);
         }
+        __syncwarp();
+        if (col + sc * 8 < g.cols) {
 #pragma unroll
-        for (int t = 0; t < TERMS; ++t) {
-            __syncwarp();
+            for (int t = 0; t < TERMS; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t h[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    float &x = v[i * 8 + 2 * k], &y = v[i * 8 + 2 * k + 1];
-                    h[k] = pack_f16x2(x, y);
-                    if (TERMS == 2 && t == 0) {
-                        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[k]));
-                        x -= f.x; y -= f.y;
-                    }
-                    if (mirror) {
-                        // an even lane gets its neighbour's entry of the first column, an odd one that of the second
-                        const uint32_t o = __shfl_xor_sync(0xffffffffu, h[k], 1);
-                        *reinterpret_cast<uint32_t*>(mir_ptr + (i * 8 + 2 * k + odd) * 64 + (lane - odd) * 2) =
-                            odd ? __byte_perm(o, h[k], 0x7632) : __byte_perm(h[k], o, 0x5410);
-                    }
-                }
-                *reinterpret_cast<uint4*>(stage_ptr + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
-            }
-            __syncwarp();
-            __half* out = g.out + base + t * g.term_stride;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = sr + 8 * i;
-                if (row_w + r < g.rows && col + sc * 8 < g.cols)
-                    *reinterpret_cast<uint4*>(out + (int64_t)(row_w + r) * g.pitch + col + sc * 8) =
-                        *reinterpret_cast<const uint4*>(stage_ptr + r * 64 + ((sc ^ ((r >> 1) & 3)) << 4));
-                if (mirror && col + r < g.cols && row_w + sc * 8 < g.rows)
-                    *reinterpret_cast<uint4*>(out + (int64_t)(col + r) * g.pitch + row_w + sc * 8) = *reinterpret_cast<const uint4*>(mir_ptr + r * 64 + sc * 16);
-            }
+                for (int i = 0; i < IT; ++i)
+                    if (row_w + sr + RPI * i < g.rows)
+                        *reinterpret_cast<uint4*>(g.img + t * g.term + lane_at + RPI * i * g.pitch + q * W) =
+                            *reinterpret_cast<const uint4*>(stage_ptr + at(t, sr + RPI * i, sc));
         }
+        __syncwarp();
     }
 }
 
 // The same rows and columns -> the caller's matrix, along rows: 8 entries a lane where rows start on 16-byte boundaries.
-template <class T, int NC>
-__device__ __forceinline__ void final_epilogue(const GemmArgs& g, uint32_t d, float alpha, void* X, int row_w, int lane, int col_w, unsigned char* stage_ptr) {
+struct Final {
+    void* X;
+    int64_t ld_x;
+    int rows, cols, update, x_vec;       // X <- wc X - wd D, or X <- D; x_vec: rows of X on 16-byte boundaries, and whole vectors
+    float wc, wd;
+};
+template <class T>
+__device__ __forceinline__ void final_epilogue(const Final& g, uint32_t d, float alpha, int row_w, int lane, int col_w, unsigned char* stage_ptr) {
+    void* X = g.X;
     float* blk = reinterpret_cast<float*>(stage_ptr);
     const int high = min(32, g.rows - row_w);
     constexpr int V = 16 / sizeof(T), PER = 32 / V, STEP = 32 / PER;      // entries a lane takes, lanes a row, rows a turn
@@ -500,113 +648,127 @@ __device__ __forceinline__ void final_epilogue(const GemmArgs& g, uint32_t d, fl
     }
 }
 
-template <bool PAIR, int BN, int TERMS, int EPI, class TABLE>
-__global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant__ TABLE table, const __grid_constant__ GemmArgs g) {
-    constexpr int NB = side_rows<PAIR, BN>(), STAGE = stage_bytes<PAIR, BN, TERMS>(), NS = stages<PAIR, BN, TERMS>();
-    constexpr int A_BYTES = 128 * 128 * TERMS;
-    constexpr int NC = BN / 2;                       // columns of one epilogue warp
-    constexpr uint32_t NCTA = PAIR ? 2 : 1;
-    const int crank = PAIR ? (int)cluster_ctarank() : 0;
-    const int tile0 = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x, tstep = PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x;
+template <int TERMS>
+__global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant__ Table table, const __grid_constant__ ChainArgs g) {
+    constexpr int A_BYTES = 128 * 128 * TERMS, STAGE = 2 * A_BYTES, NS = STAGE_RING / STAGE;
+    const int crank = (int)cluster_ctarank();
+    const int pair0 = (int)(blockIdx.x >> 1), pairs = (int)(gridDim.x >> 1);
 
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
     unsigned char* smem = smem_raw + (base - raw);
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + STAGE_BYTES + 8 * 4096);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + STAGE_RING + 8 * 4096);
     const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * MAX_STAGES, tfull0 = empty0 + 8 * MAX_STAGES, tempty0 = tfull0 + 16;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * MAX_STAGES + 4);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < NS; ++s) { mbar_init(full0 + 8 * s, NCTA); mbar_init(empty0 + 8 * s, 1); }
-        for (int a = 0; a < 2; ++a) { mbar_init(tfull0 + 8 * a, 1); mbar_init(tempty0 + 8 * a, NCTA * 8); }
+        for (int s = 0; s < NS; ++s) { mbar_init(full0 + 8 * s, 2); mbar_init(empty0 + 8 * s, 1); }
+        for (int a = 0; a < 2; ++a) { mbar_init(tfull0 + 8 * a, 1); mbar_init(tempty0 + 8 * a, 2 * 8); }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_smem();
-        prefetch_tensor_map(&g.map_a);
-        prefetch_tensor_map(&g.map_b);
     }
-    if (warp == 1) {
-        if (PAIR) tmem_alloc_pair(smem_u32(tmem_slot), 2 * BN);
-        else tmem_alloc(smem_u32(tmem_slot), 2 * BN);
-    }
-    grid_dependency_launch();
+    if (warp == 1) tmem_alloc_pair(smem_u32(tmem_slot), 2 * TM);
     tc_fence_before();
     __syncthreads();
-    if (PAIR) cluster_sync_all();       // the peer's barriers are initialised before anything reaches them
+    cluster_sync_all();                 // the peer's barriers are initialised before anything reaches them
     tc_fence_after();
-    grid_dependency_wait();
+    grid_dependency();
     const uint32_t tmem_base = *tmem_slot;
-    const uint32_t full_ld = PAIR ? map_to_rank(full0, 0) : full0, tempty_ld = PAIR ? map_to_rank(tempty0, 0) : tempty0;
+    const uint32_t full_ld = map_to_rank(full0, 0), tempty_ld = map_to_rank(tempty0, 0);
+    Walk w{0, 0, 0, pair0};
+    Unit u;
 
     if (warp == 0) {
         // ---------------- producer: this CTA's rows of A and of B, both planes of a 64-deep block per stage ----------------
-        if (lane == 0) {
-            int s = 0; uint32_t ph = 0;
-            bool ok = true;
-            for (int t = tile0; t < g.total && ok; t += tstep) {
-                const Tile c = decode<PAIR, BN>(g, t);
-                if (!c.active) continue;
-                const int ar = c.row0 + crank * 128, br = c.col0 + crank * NB;
-                for (int kb = 0; kb < g.kblocks; ++kb) {
-                    if (!mbar_wait(empty0 + 8 * s, ph ^ 1, abort_flag)) { ok = false; break; }
-                    const uint32_t fb = full_ld + 8 * s, dst = base + s * STAGE;
-                    if (PAIR) mbar_arrive_expect_tx_remote(fb, STAGE);
-                    else mbar_arrive_expect_tx(fb, STAGE);
-                    if (g.a_mn) {
-                        tma_load4(dst, &g.map_a, ar, kb * 64, 0, c.mat, fb, PAIR);
-                        tma_load4(dst + 8192 * TERMS, &g.map_a, ar + 64, kb * 64, 0, c.mat, fb, PAIR);
-                    } else {
-                        tma_load4(dst, &g.map_a, kb * 64, ar, 0, c.mat, fb, PAIR);
+        // The whole warp asks for the counts of the next 32 tiles of either side; lane 0 issues the loads.
+        int s = 0; uint32_t ph = 0;
+        bool ok = true;
+        for (; ok && find_unit(g, w, u); w.unit += pairs) {
+            const Class& c = g.c[u.cls];
+            Side a, b;
+            sides_of(c, u, a, b);
+            const uint32_t* counts = c.tile_done + (int64_t)u.mat * c.counts;
+            const uint32_t want_a = ARRIVALS * writes_of(c, u.op, a.image), want_b = ARRIVALS * writes_of(c, u.op, b.image);
+            const CUtensorMap *ka = a.image < 4 ? &c.k_sq[a.image] : &c.k_x[a.image - 4], *kb_ = b.image < 4 ? &c.k_sq[b.image] : &c.k_x[b.image - 4];
+            const CUtensorMap *ma = a.image < 4 ? &c.mn_sq[a.image] : &c.mn_x[a.image - 4], *mb = b.image < 4 ? &c.mn_sq[b.image] : &c.mn_x[b.image - 4];
+            const int ar = u.ti * TM + crank * 128, br = u.tj * TM + crank * 128;
+            int ready = u.stage ? 0 : u.kblocks;          // depth blocks whose tiles are known to be there (X's first image is, from the start)
+            for (int kb = 0; kb < u.kblocks; ++kb) {
+                if (kb >= ready) {
+                    const long long t0 = clock64();
+                    for (int spins = 0; ok; ++spins) {
+                        const int k = kb + 4 * lane;
+                        bool there = k >= u.kblocks;
+                        if (!there)
+                            there = (int32_t)(load_acquire(counts + a.place(c, k)) - want_a) >= 0 && (int32_t)(load_acquire(counts + b.place(c, k)) - want_b) >= 0;
+                        const uint32_t missing = __ballot_sync(0xffffffffu, !there);
+                        ready = kb + 4 * (missing ? __ffs(missing) - 1 : 32);
+                        if (ready > kb) break;
+                        if ((spins & 15) == 15 && (*abort_flag || clock64() - t0 > WAIT_LIMIT_CYCLES)) { *abort_flag = 1; ok = false; }
+                        ok = __all_sync(0xffffffffu, ok);
+                        __nanosleep(20);
                     }
-                    if (g.b_mn) {
-#pragma unroll
-                        for (int q = 0; q < NB / 64; ++q)
-                            tma_load4(dst + A_BYTES + q * 8192 * TERMS, &g.map_b, br + q * 64, kb * 64, 0, c.mat, fb, PAIR);
-                    } else {
-                        tma_load4(dst + A_BYTES, &g.map_b, kb * 64, br, 0, c.mat, fb, PAIR);
-                    }
-                    if (++s == NS) { s = 0; ph ^= 1; }
+                    if (!ok) break;
+                    asm volatile("fence.proxy.async;" ::: "memory");
+                    __syncwarp();
                 }
+                if (lane == 0) {
+                    ok = mbar_wait(empty0 + 8 * s, ph ^ 1, abort_flag);
+                    if (ok) {
+                        const uint32_t fb = full_ld + 8 * s, dst = base + s * STAGE;
+                        mbar_arrive_expect_tx_remote(fb, STAGE);
+                        if (a.along_columns(kb)) tma_load_mn(dst, ma, kb * 64, ar / 64, u.mat, fb);
+                        else tma_load_k(dst, ka, kb * 64, ar, u.mat, fb);
+                        if (b.along_columns(kb)) tma_load_mn(dst + A_BYTES, mb, kb * 64, br / 64, u.mat, fb);
+                        else tma_load_k(dst + A_BYTES, kb_, kb * 64, br, u.mat, fb);
+                    }
+                }
+                ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+                if (!ok) break;
+                if (++s == NS) { s = 0; ph ^= 1; }
             }
         }
         __syncwarp();
     } else if (warp == 1) {
         // ---------------- MMA issuer ----------------
         if (lane == 0 && crank == 0) {
-            const uint32_t a_step = g.a_mn ? (2048u >> 4) : (32u >> 4), b_step = g.b_mn ? (2048u >> 4) : (32u >> 4);     // one 16-deep slice
-            const uint32_t a_term = g.a_mn ? (8192u >> 4) : (16384u >> 4), b_term = g.b_mn ? (8192u >> 4) : (uint32_t)(NB * 128) >> 4;
-            const uint64_t a_desc = g.a_mn ? smem_desc(0, 8192 * TERMS, 1024) : smem_desc(0, 16, 1024);
-            const uint64_t b_desc = g.b_mn ? smem_desc(0, 8192 * TERMS, 1024) : smem_desc(0, 16, 1024);
-            const uint32_t a_hi = (uint32_t)(a_desc >> 32), b_hi = (uint32_t)(b_desc >> 32);
-            const uint32_t a0 = (uint32_t)a_desc + (base >> 4), b0 = (uint32_t)b_desc + ((base + A_BYTES) >> 4);
-            const uint32_t idesc = instr_desc(BN, g.a_mn, g.b_mn, 0u, PAIR ? 256u : 128u);
+            // operand tiles along rows: rows of 128 bytes, eight of them 1024 bytes apart; along columns: 64-column groups 8192 bytes apart
+            const uint64_t k_desc = smem_desc(0, 16, 1024), mn_desc = smem_desc(0, 8192, 1024);
+            const uint32_t d_hi = (uint32_t)(k_desc >> 32);             // (both forms')
+            const uint32_t k_lo = (uint32_t)k_desc + (base >> 4), mn_lo = (uint32_t)mn_desc + (base >> 4);
+            constexpr uint32_t TERM = 16384u >> 4, B_AT = (uint32_t)A_BYTES >> 4;
             int s = 0, acc = 0; uint32_t ph = 0, aph = 0;
             bool ok = true;
-            for (int t = tile0; t < g.total && ok; t += tstep) {
-                if (!decode<PAIR, BN>(g, t).active) continue;
-                for (int k0 = 0; k0 < g.kblocks && ok; k0 += g.chunk) {
+            for (; ok && find_unit(g, w, u); w.unit += pairs) {
+                Side sa, sb;
+                sides_of(g.c[u.cls], u, sa, sb);
+                const int chunk = TERMS == 2 ? 1 : u.kblocks;          // depth blocks that are summed in tensor memory
+                for (int k0 = 0; k0 < u.kblocks && ok; k0 += chunk) {
                     if (!mbar_wait(tempty0 + 8 * acc, aph ^ 1, abort_flag)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t d = tmem_base + acc * BN;
-                    const int k1 = min(g.kblocks, k0 + g.chunk);
-                    for (int kb = k0; kb < k1; ++kb) {
+                    const uint32_t d = tmem_base + acc * TM;
+                    for (int kb = k0; kb < k0 + chunk; ++kb) {
                         if (!mbar_wait(full0 + 8 * s, ph, abort_flag)) { ok = false; break; }
-                        const uint32_t off = (uint32_t)(s * STAGE) >> 4;
+                        const bool a_mn = sa.along_columns(kb), b_mn = sb.along_columns(kb);
+                        const uint32_t off = (uint32_t)(s * STAGE) >> 4, a = off + (a_mn ? mn_lo : k_lo), b = off + B_AT + (b_mn ? mn_lo : k_lo);
+                        const uint32_t a_step = a_mn ? (2048u >> 4) : (32u >> 4), b_step = b_mn ? (2048u >> 4) : (32u >> 4);     // one 16-deep slice
+                        const uint32_t idesc = instr_desc(TM, a_mn, b_mn, 0u, 256u);
                         if (TERMS == 2) {
                             // the small products first: an addition truncates at the accumulator's size of the moment
-                            umma_slices<PAIR, 4, false>(d, a0 + off, a_hi, b0 + off + b_term, b_hi, a_step, b_step, 0, 0, idesc, kb > k0 ? 1u : 0u);
-                            umma_slices<PAIR, 4, false>(d, a0 + off + a_term, a_hi, b0 + off, b_hi, a_step, b_step, 0, 0, idesc, 1u);
-                            umma_slices<PAIR, 4, false>(d, a0 + off, a_hi, b0 + off, b_hi, a_step, b_step, 0, 0, idesc, 1u);
+                            umma_slices<true, 4, false>(d, a, d_hi, b + TERM, d_hi, a_step, b_step, 0, 0, idesc, 0u);
+                            umma_slices<true, 4, false>(d, a + TERM, d_hi, b, d_hi, a_step, b_step, 0, 0, idesc, 1u);
+                            umma_slices<true, 4, false>(d, a, d_hi, b, d_hi, a_step, b_step, 0, 0, idesc, 1u);
                         } else {
-                            umma_slices<PAIR, 4, false>(d, a0 + off, a_hi, b0 + off, b_hi, a_step, b_step, 0, 0, idesc, kb > k0 ? 1u : 0u);
+                            umma_slices<true, 4, false>(d, a, d_hi, b, d_hi, a_step, b_step, 0, 0, idesc, kb > k0 ? 1u : 0u);
                         }
-                        commit_any<PAIR>(empty0 + 8 * s);
+                        commit_any<true>(empty0 + 8 * s);
                         if (++s == NS) { s = 0; ph ^= 1; }
                     }
                     if (!ok) break;
-                    commit_any<PAIR>(tfull0 + 8 * acc);
+                    commit_any<true>(tfull0 + 8 * acc);
                     if (++acc == 2) { acc = 0; aph ^= 1; }
                 }
             }
@@ -615,15 +777,24 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
     } else {
         // ---------------- epilogue: warp w has the 32 rows that its tensor-memory quarter holds, and half the columns ----------------
         const int quarter = warp % 4, half = (warp - 2) / 4;
-        unsigned char* stage_ptr = smem + STAGE_BYTES + (warp - 2) * 4096;
+        unsigned char* stage_ptr = smem + STAGE_RING + (warp - 2) * 4096;
         int acc = 0; uint32_t aph = 0;
         bool ok = true;
-        for (int t = tile0; t < g.total && ok; t += tstep) {
-            const Tile c = decode<PAIR, BN>(g, t);
-            if (!c.active) continue;
-            const int row_w = c.row0 + crank * 128 + quarter * 32, col_w = c.col0 + half * NC;
-            const bool mine = row_w < g.rows && col_w < g.cols;
-            const uint32_t mine_tmem = tmem_base + half * NC + ((uint32_t)(quarter * 32) << 16);
+        const uint32_t mine_tmem = tmem_base + half * NC + ((uint32_t)(quarter * 32) << 16);
+        auto release = [&] {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_remote(tempty_ld + 8 * acc);
+            if (++acc == 2) { acc = 0; aph ^= 1; }
+        };
+        for (; find_unit(g, w, u); w.unit += pairs) {
+            // no unit of the product before the last reads any more what will be written here
+            if (u.op.out >= 0 && u.stage >= 2) {
+                const Class& c = g.c[u.cls];
+                const uint32_t want = ARRIVALS * units_before(c, u.stage - 1, op_of(c, u.stage - 1).group);
+                ok = __all_sync(0xffffffffu, wait_count(&c.slot[u.mat].done, want, abort_flag));
+                if (!ok) break;
+            }
             if (TERMS == 1) {
                 // (all lanes alike: a wait that ran out for one ends the warp's work)
                 ok = __all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * acc, aph, abort_flag));
@@ -635,50 +806,73 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                 float v[NC];
 #pragma unroll
                 for (int e = 0; e < NC; ++e) v[e] = 0.f;
-                int left = (g.kblocks + g.chunk - 1) / g.chunk;
+                int left = u.kblocks;
                 while (true) {
                     ok = __all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * acc, aph, abort_flag));
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t d = mine_tmem + acc * BN;
+                    const uint32_t d = mine_tmem + acc * TM;
 #pragma unroll
                     for (int q = 0; q < NC / 16; ++q) {
-                        uint32_t u[16];
-                        tmem_ld16(d + q * 16, u);
+                        uint32_t x[16];
+                        tmem_ld16(d + q * 16, x);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) v[q * 16 + e] += __uint_as_float(u[e]);
+                        for (int e = 0; e < 16; ++e) v[q * 16 + e] += __uint_as_float(x[e]);
                     }
                     if (--left == 0) break;
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) { if (PAIR) mbar_arrive_remote(tempty_ld + 8 * acc); else mbar_arrive(tempty0 + 8 * acc); }
-                    if (++acc == 2) { acc = 0; aph ^= 1; }
+                    release();
                 }
                 if (!ok) break;
-                const uint32_t d = mine_tmem + acc * BN;
+                const uint32_t d = mine_tmem + acc * TM;
 #pragma unroll
                 for (int q = 0; q < NC / 16; ++q) tmem_st16(d + q * 16, &v[q * 16]);
                 tmem_st_wait();
+                find_unit(g, w, u);        // (once more, in place of the registers that it would hold across the sums)
             }
-            const uint32_t d = mine_tmem + acc * BN;
-            float alpha = g.alpha;
-            if (g.sigma_pow) {
-                const float sg = g.slot[c.mat].sigma;
-                alpha *= g.sigma_pow == 2 ? sg * sg : sg;
-            }
-            if constexpr (EPI == EPI_IMAGE) {
-                if (mine) image_epilogue<TERMS, NC>(g, d, alpha, c.mat, row_w, lane, col_w, c.mirror, stage_ptr);
-            } else {
-                if (mine && !g.slot[c.mat].status) {
-                    if (g.x_bf16) final_epilogue<__nv_bfloat16, NC>(g, d, alpha, table.w[c.mat].X, row_w, lane, col_w, stage_ptr);
-                    else final_epilogue<float, NC>(g, d, alpha, table.w[c.mat].X, row_w, lane, col_w, stage_ptr);
+            const Class& c = g.c[u.cls];
+            const Slot* slot = &c.slot[u.mat];
+            const int row_w = u.ti * TM + crank * 128 + quarter * 32, col_w = u.tj * TM + half * NC;
+            const uint32_t d = mine_tmem + acc * TM;
+            const bool apply = u.op.kind == OP_APPLY;
+            if (row_w < u.rows && col_w < u.cols) {
+                float alpha = 1.f / UNIT;
+                // the images hold UNIT times the value, the first one of X divided by sigma
+                if (u.op.group == 0 && u.op.kind == OP_GRAM) { const float sg = __ldcg(&slot->sigma); alpha *= sg * sg; }
+                if (u.op.group == 0 && apply) alpha *= __ldcg(&slot->sigma);
+                if (u.op.out >= 0) {
+                    Out o;
+                    const int64_t at = u.mat * (apply ? c.x_mat : c.s_mat);
+                    o.img = (apply ? c.x[u.op.out - 4] : c.sq[u.op.out]) + at;
+                    o.pitch = apply ? c.x_pitch : c.s_pitch; o.term = apply ? c.x_term : c.s_term;
+                    o.rows = u.rows; o.cols = u.cols;
+                    o.add = nullptr;
+                    if (u.op.kind == OP_POLY) {
+                        const float* k = c.abc[u.op.step];
+                        alpha *= k[2];
+                        o.beta = k[1]; o.diag = k[0] * UNIT;
+                        o.add = c.sq[u.op.a] + at;
+                    }
+                    image_epilogue<TERMS>(o, d, alpha, row_w, lane, col_w, stage_ptr);
+                } else if (!__ldcg(&slot->status)) {
+                    const Final f{table.w[c.first + u.mat].X, c.ld_x, u.rows, u.cols, c.update, c.x_vec, c.wc, c.wd};
+                    if (c.x_bf16) final_epilogue<__nv_bfloat16>(f, d, alpha / UNIT, row_w, lane, col_w, stage_ptr);
+                    else final_epilogue<float>(f, d, alpha / UNIT, row_w, lane, col_w, stage_ptr);
                 }
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) { if (PAIR) mbar_arrive_remote(tempty_ld + 8 * acc); else mbar_arrive(tempty0 + 8 * acc); }
-            if (++acc == 2) { acc = 0; aph ^= 1; }
+            release();
+            if (u.op.out >= 0) {
+                // every lane's stores before the counts (which release them, by way of lane 0)
+                __syncwarp();
+                if (lane == 0) {
+                    const int place = u.op.out < 4 ? u.op.out * c.tiles_sq + u.ti * (u.ti + 1) / 2 + u.tj
+                                                   : 4 * c.tiles_sq + (u.op.out - 4) * c.tiles_x + u.ti * tiles_along(c.n) + u.tj;
+                    asm volatile("fence.proxy.async;" ::: "memory");
+                    asm volatile("fence.acq_rel.gpu;" ::: "memory");
+                    asm volatile("red.relaxed.gpu.global.add.u32 [%0], 1;" ::"l"(c.tile_done + (int64_t)u.mat * c.counts + place) : "memory");
+                    asm volatile("red.relaxed.gpu.global.add.u32 [%0], 1;" ::"l"(&c.slot[u.mat].done) : "memory");
+                }
+            }
         }
     }
 
@@ -691,23 +885,11 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
     }
     tc_fence_before();
     __syncthreads();
-    if (PAIR) cluster_sync_all();
+    cluster_sync_all();
     tc_fence_after();
-    if (threadIdx.x == 0) {
-        if (*abort_flag)
-            for (int i = 0; i < g.count; ++i) atomicOr(&g.slot[i].status, ST_WAIT);
-        if constexpr (EPI == EPI_FINAL) {
-            if (*abort_flag || blockIdx.x == 0)
-                for (int i = 0; i < g.count; ++i) {
-                    const int st = *abort_flag ? ST_WAIT : g.slot[i].status;
-                    if (st) atomicOr(table.w[i].status, st);
-                }
-        }
-    }
-    if (warp == 1) {
-        if (PAIR) tmem_dealloc_pair(tmem_base, 2 * BN);
-        else tmem_dealloc(tmem_base, 2 * BN);
-    }
+    if (*abort_flag && threadIdx.x == 0)
+        for (int i = 0; i < table.count; ++i) atomicOr(table.w[i].status, ST_WAIT);
+    if (warp == 1) tmem_dealloc_pair(tmem_base, 2 * TM);
 }
 
 }  // namespace ns
