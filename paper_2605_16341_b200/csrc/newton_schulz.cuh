@@ -250,9 +250,13 @@ __global__ void __launch_bounds__(256) prep_kernel(const __grid_constant__ Table
 // 768 x 2048, and multiprocessors without work at the end of each.  One kernel that waits for whole products: 15 of 80 us, the results'
 // stores and their fences among them.)
 constexpr int STAGE_RING = 196608;            // bytes of the operand ring
-constexpr int THREADS = 32 * 10;              // producer, issuer, eight epilogue warps
+// Three warpgroups: scout, producer and issuer (and a warp without work), and eight epilogue warps, which take most of the registers that the first
+// gives back: 128 x 80 + 256 x 208 of the 384 x 168 that the block is launched with.
+constexpr int THREADS = 384, FEW_REGS = 80, MANY_REGS = 208;
+static_assert(128 * FEW_REGS + 256 * MANY_REGS <= THREADS * 168, "registers");
 constexpr int MAX_STAGES = 6;
-constexpr int SMEM_BYTES = 1024 + STAGE_RING + 8 * 4096 + 256;
+constexpr int UNITS = 4;                      // that the scout is ahead of the epilogue at most
+constexpr int SMEM_BYTES = 1024 + STAGE_RING + 8 * 4096 + 256 + UNITS * 128;      // operands, epilogue blocks, barriers, units
 constexpr int TM = 256;                       // rows (128 of each CTA of a pair) and columns of a tile
 constexpr int NC = TM / 2;                    // columns of an epilogue warp
 constexpr int GROUP_ROWS = 8;                 // tile rows that are walked together, column by column
@@ -341,6 +345,8 @@ struct Unit {
     int cls, mat, stage;
     int ti, tj, rows, cols, kblocks;          // tile row and column
     Op op;
+    int a_turn, b_turn;                       // depth block from which on a side is read along its columns
+    const CUtensorMap *k_a, *k_b, *mn_a, *mn_b;
 };
 // Makes w.unit a unit of (w.stage, w.cls), or returns false behind the last.
 __device__ __forceinline__ bool find_unit(const ChainArgs& g, Walk& w, Unit& u) {
@@ -420,7 +426,6 @@ struct Side {
     int image, tile;
     bool sym;              // a symmetric image: mirrored above the diagonal
     bool mn;               // X along its columns: depth runs down its rows
-    __device__ __forceinline__ bool along_columns(int kb) const { return sym ? kb / 4 > tile : mn; }
     // index of the tile of depth block kb in its image's counts
     __device__ __forceinline__ int place(const Class& c, int kb) const {
         const int k = kb / 4;
@@ -446,6 +451,11 @@ __device__ __forceinline__ void sides_of(const Class& c, const Unit& u, Side& a,
 __device__ __forceinline__ uint32_t load_acquire(const uint32_t* p) {
     uint32_t v;
     asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t load_relaxed(const uint32_t* p) {
+    uint32_t v;
+    asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
     return v;
 }
 // Waits until a count has come to `want`; then what was written before it was raised can be read.
@@ -586,7 +596,6 @@ __device__ __forceinline__ void final_epilogue(const Final& g, uint32_t d, float
             if (r < high && col + vc < g.cols) old[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(X) + (int64_t)(row_w + r) * g.ld_x + col + vc);
         }
     };
-    if (g.x_vec && g.update) fetch(col_w);
 #pragma unroll 1
     for (int q = 0; q < NC / 32; ++q) {
         const int col = col_w + q * 32;
@@ -604,6 +613,7 @@ __device__ __forceinline__ void final_epilogue(const Final& g, uint32_t d, float
             __syncwarp();
         }
         if (g.x_vec) {
+            if (g.update) fetch(col);
 #pragma unroll
             for (int i = 0; i < 32 / STEP; ++i) {
                 const int r = vr + i * STEP;
@@ -626,19 +636,18 @@ __device__ __forceinline__ void final_epilogue(const Final& g, uint32_t d, float
                 if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(x) = make_float4(v[0], v[1], v[2], v[3]);
                 else *reinterpret_cast<uint4*>(x) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
             }
-            if (g.update && q + 1 < NC / 32) fetch(col + 32);
         } else if (col + lane < g.cols) {
             T* x = reinterpret_cast<T*>(X) + (int64_t)row_w * g.ld_x + col + lane;
-            // (sixteen loads under way: stores to X in between would hold each of them back)
+            // (eight loads under way: stores to X in between would hold each of them back)
 #pragma unroll 1
-            for (int r0 = 0; r0 < high; r0 += 16) {
-                float x0[16];
+            for (int r0 = 0; r0 < high; r0 += 8) {
+                float x0[8];
                 if (g.update) {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) x0[r] = r0 + r < high ? to_float(x[(r0 + r) * g.ld_x]) : 0.f;
+                    for (int r = 0; r < 8; ++r) x0[r] = r0 + r < high ? to_float(x[(r0 + r) * g.ld_x]) : 0.f;
                 }
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
+                for (int r = 0; r < 8; ++r) {
                     const float f = blk[(r0 + r) * 32 + (lane ^ ((r & 7) * 4))];
                     if (r0 + r < high) x[(r0 + r) * g.ld_x] = from_float<T>(g.update ? g.wc * x0[r] - g.wd * f : f);
                 }
@@ -659,13 +668,17 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
     unsigned char* smem = smem_raw + (base - raw);
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + STAGE_RING + 8 * 4096);
     const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * MAX_STAGES, tfull0 = empty0 + 8 * MAX_STAGES, tempty0 = tfull0 + 16;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * MAX_STAGES + 4);
+    const uint32_t ufull0 = tempty0 + 16, uempty0 = ufull0 + 8 * UNITS;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * MAX_STAGES + 4 + 2 * UNITS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    const uint32_t ready_at = smem_u32(tmem_slot + 2);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < NS; ++s) { mbar_init(full0 + 8 * s, 2); mbar_init(empty0 + 8 * s, 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(tfull0 + 8 * a, 1); mbar_init(tempty0 + 8 * a, 2 * 8); }
+        for (int e = 0; e < UNITS; ++e) { mbar_init(ufull0 + 8 * e, 1); mbar_init(uempty0 + 8 * e, 8); }
+        tmem_slot[2] = 0;
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_smem();
@@ -678,57 +691,112 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
     grid_dependency();
     const uint32_t tmem_base = *tmem_slot;
     const uint32_t full_ld = map_to_rank(full0, 0), tempty_ld = map_to_rank(tempty0, 0);
-    Walk w{0, 0, 0, pair0};
-    Unit u;
+    // The scout's units, each until the epilogue warps are through with it; and how many depth blocks of all units so far it has found there.
+    Unit* ring = reinterpret_cast<Unit*>(smem + STAGE_RING + 8 * 4096 + 256);
+    static_assert(sizeof(Unit) <= 128, "units in shared memory");
+    auto unit_at = [&](int e) { return reinterpret_cast<Unit*>(reinterpret_cast<unsigned char*>(ring) + e * 128); };
 
-    if (warp == 0) {
-        // ---------------- producer: this CTA's rows of A and of B, both planes of a 64-deep block per stage ----------------
-        // The whole warp asks for the counts of the next 32 tiles of either side; lane 0 issues the loads.
-        int s = 0; uint32_t ph = 0;
+    if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(FEW_REGS));
+    if (warp == 2) {
+        // ---------------- scout: finds this pair's units, and waits for their operands' tiles, 32 of either side at a time ----------------
+        // (by the producer, between two units or ahead of the last loads of one, this cost the MMAs 1.5 to 2 us a unit)
+        Walk w{0, 0, 0, pair0};
+        int e = 0, total = 0; uint32_t eph = 0;
         bool ok = true;
-        for (; ok && find_unit(g, w, u); w.unit += pairs) {
+        while (ok) {
+            ok = __all_sync(0xffffffffu, mbar_wait(uempty0 + 8 * e, eph ^ 1, abort_flag));
+            if (!ok) break;
+            Unit& u = *unit_at(e);
+            int more = 0;
+            if (lane == 0) {
+                more = find_unit(g, w, u);
+                w.unit += pairs;
+                if (more) {
+                    const Class& c = g.c[u.cls];
+                    Side a, b;
+                    sides_of(c, u, a, b);
+                    u.a_turn = a.sym ? 4 * (a.tile + 1) : a.mn ? 0 : u.kblocks;
+                    u.b_turn = b.sym ? 4 * (b.tile + 1) : b.mn ? 0 : u.kblocks;
+                    u.k_a = a.image < 4 ? &c.k_sq[a.image] : &c.k_x[a.image - 4];
+                    u.k_b = b.image < 4 ? &c.k_sq[b.image] : &c.k_x[b.image - 4];
+                    u.mn_a = a.image < 4 ? &c.mn_sq[a.image] : &c.mn_x[a.image - 4];
+                    u.mn_b = b.image < 4 ? &c.mn_sq[b.image] : &c.mn_x[b.image - 4];
+                } else {
+                    u.kblocks = 0;                 // the end
+                }
+                mbar_arrive(ufull0 + 8 * e);
+            }
+            more = __shfl_sync(0xffffffffu, more, 0);
+            if (!more) break;
             const Class& c = g.c[u.cls];
             Side a, b;
             sides_of(c, u, a, b);
             const uint32_t* counts = c.tile_done + (int64_t)u.mat * c.counts;
             const uint32_t want_a = ARRIVALS * writes_of(c, u.op, a.image), want_b = ARRIVALS * writes_of(c, u.op, b.image);
-            const CUtensorMap *ka = a.image < 4 ? &c.k_sq[a.image] : &c.k_x[a.image - 4], *kb_ = b.image < 4 ? &c.k_sq[b.image] : &c.k_x[b.image - 4];
-            const CUtensorMap *ma = a.image < 4 ? &c.mn_sq[a.image] : &c.mn_x[a.image - 4], *mb = b.image < 4 ? &c.mn_sq[b.image] : &c.mn_x[b.image - 4];
-            const int ar = u.ti * TM + crank * 128, br = u.tj * TM + crank * 128;
-            int ready = u.stage ? 0 : u.kblocks;          // depth blocks whose tiles are known to be there (X's first image is, from the start)
-            for (int kb = 0; kb < u.kblocks; ++kb) {
-                if (kb >= ready) {
+            const int kblocks = u.kblocks;
+            const long long t0 = clock64();
+            for (int kb = 0, spins = 0; kb < kblocks; ++spins) {
+                const int k = kb + 4 * lane;
+                bool there = true;
+                if (k < kblocks) {
+                    const uint32_t x = load_relaxed(counts + a.place(c, k)), y = load_relaxed(counts + b.place(c, k));
+                    there = (int32_t)(x - want_a) >= 0 && (int32_t)(y - want_b) >= 0;
+                }
+                const uint32_t missing = __ballot_sync(0xffffffffu, !there);
+                const int tiles = missing ? __ffs(missing) - 1 : 32;
+                if (tiles) {
+                    asm volatile("fence.acq_rel.gpu;" ::: "memory");
+                    asm volatile("fence.proxy.async;" ::: "memory");
+                    __syncwarp();
+                    kb = min(kblocks, kb + 4 * tiles);
+                    if (lane == 0) asm volatile("st.release.cta.shared::cta.u32 [%0], %1;" ::"r"(ready_at), "r"(total + kb) : "memory");
+                } else {
+                    if ((spins & 15) == 15 && (*abort_flag || clock64() - t0 > WAIT_LIMIT_CYCLES)) { *abort_flag = 1; ok = false; }
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    __nanosleep(20);
+                }
+            }
+            total += kblocks;
+            if (++e == UNITS) { e = 0; eph ^= 1; }
+        }
+    } else if (warp == 0) {
+        // ---------------- producer: this CTA's rows of A and of B, both planes of a 64-deep block per stage ----------------
+        // (one thread's loop over blocks of one kind, with nothing in it that could be outside: at 1000 cycles a turn it was what bounded the MMAs)
+        if (lane == 0) {
+            int s = 0, e = 0, total = 0, ready = 0; uint32_t ph = 0, eph = 0;
+            bool ok = true;
+            while (ok && mbar_wait(ufull0 + 8 * e, eph, abort_flag)) {
+                const Unit& u = *unit_at(e);
+                const int kblocks = u.kblocks, mat = u.mat, a_turn = u.a_turn, b_turn = u.b_turn;
+                if (!kblocks) break;
+                const CUtensorMap *ka = u.k_a, *kb_ = u.k_b, *ma = u.mn_a, *mb = u.mn_b;
+                const int ar = u.ti * TM + crank * 128, br = u.tj * TM + crank * 128;
+                for (int kb = 0; kb < kblocks && ok;) {
                     const long long t0 = clock64();
-                    for (int spins = 0; ok; ++spins) {
-                        const int k = kb + 4 * lane;
-                        bool there = k >= u.kblocks;
-                        if (!there)
-                            there = (int32_t)(load_acquire(counts + a.place(c, k)) - want_a) >= 0 && (int32_t)(load_acquire(counts + b.place(c, k)) - want_b) >= 0;
-                        const uint32_t missing = __ballot_sync(0xffffffffu, !there);
-                        ready = kb + 4 * (missing ? __ffs(missing) - 1 : 32);
-                        if (ready > kb) break;
-                        if ((spins & 15) == 15 && (*abort_flag || clock64() - t0 > WAIT_LIMIT_CYCLES)) { *abort_flag = 1; ok = false; }
-                        ok = __all_sync(0xffffffffu, ok);
-                        __nanosleep(20);
+                    for (int spins = 0; ready <= total + kb; ++spins) {
+                        asm volatile("ld.acquire.cta.shared::cta.u32 %0, [%1];" : "=r"(ready) : "r"(ready_at) : "memory");
+                        if ((spins & 63) == 63 && (*abort_flag || clock64() - t0 > WAIT_LIMIT_CYCLES)) { *abort_flag = 1; ok = false; break; }
                     }
                     if (!ok) break;
                     asm volatile("fence.proxy.async;" ::: "memory");
-                    __syncwarp();
-                }
-                if (lane == 0) {
-                    ok = mbar_wait(empty0 + 8 * s, ph ^ 1, abort_flag);
-                    if (ok) {
+                    int end = min(ready - total, kblocks);
+                    if (kb < a_turn) end = min(end, a_turn);
+                    if (kb < b_turn) end = min(end, b_turn);
+                    const bool a_mn = kb >= a_turn, b_mn = kb >= b_turn;
+                    for (; kb < end; ++kb) {
+                        if (!mbar_wait(empty0 + 8 * s, ph ^ 1, abort_flag)) { ok = false; break; }
                         const uint32_t fb = full_ld + 8 * s, dst = base + s * STAGE;
                         mbar_arrive_expect_tx_remote(fb, STAGE);
-                        if (a.along_columns(kb)) tma_load_mn(dst, ma, kb * 64, ar / 64, u.mat, fb);
-                        else tma_load_k(dst, ka, kb * 64, ar, u.mat, fb);
-                        if (b.along_columns(kb)) tma_load_mn(dst + A_BYTES, mb, kb * 64, br / 64, u.mat, fb);
-                        else tma_load_k(dst + A_BYTES, kb_, kb * 64, br, u.mat, fb);
+                        if (a_mn) tma_load_mn(dst, ma, kb * 64, ar / 64, mat, fb);
+                        else tma_load_k(dst, ka, kb * 64, ar, mat, fb);
+                        if (b_mn) tma_load_mn(dst + A_BYTES, mb, kb * 64, br / 64, mat, fb);
+                        else tma_load_k(dst + A_BYTES, kb_, kb * 64, br, mat, fb);
+                        if (++s == NS) { s = 0; ph ^= 1; }
                     }
                 }
-                ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
-                if (!ok) break;
-                if (++s == NS) { s = 0; ph ^= 1; }
+                total += kblocks;
+                if (++e == UNITS) { e = 0; eph ^= 1; }
             }
         }
         __syncwarp();
@@ -740,19 +808,20 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
             const uint32_t d_hi = (uint32_t)(k_desc >> 32);             // (both forms')
             const uint32_t k_lo = (uint32_t)k_desc + (base >> 4), mn_lo = (uint32_t)mn_desc + (base >> 4);
             constexpr uint32_t TERM = 16384u >> 4, B_AT = (uint32_t)A_BYTES >> 4;
-            int s = 0, acc = 0; uint32_t ph = 0, aph = 0;
+            int s = 0, acc = 0, e = 0; uint32_t ph = 0, aph = 0, eph = 0;
             bool ok = true;
-            for (; ok && find_unit(g, w, u); w.unit += pairs) {
-                Side sa, sb;
-                sides_of(g.c[u.cls], u, sa, sb);
-                const int chunk = TERMS == 2 ? 1 : u.kblocks;          // depth blocks that are summed in tensor memory
-                for (int k0 = 0; k0 < u.kblocks && ok; k0 += chunk) {
+            while (ok && mbar_wait(ufull0 + 8 * e, eph, abort_flag)) {
+                const Unit& u = *unit_at(e);
+                const int kblocks = u.kblocks, chunk = TERMS == 2 ? 1 : kblocks, a_turn = u.a_turn, b_turn = u.b_turn;   // chunk: depth blocks that are summed in tensor memory
+                if (!kblocks) break;
+                if (++e == UNITS) { e = 0; eph ^= 1; }
+                for (int k0 = 0; k0 < kblocks && ok; k0 += chunk) {
                     if (!mbar_wait(tempty0 + 8 * acc, aph ^ 1, abort_flag)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t d = tmem_base + acc * TM;
                     for (int kb = k0; kb < k0 + chunk; ++kb) {
                         if (!mbar_wait(full0 + 8 * s, ph, abort_flag)) { ok = false; break; }
-                        const bool a_mn = sa.along_columns(kb), b_mn = sb.along_columns(kb);
+                        const bool a_mn = kb >= a_turn, b_mn = kb >= b_turn;
                         const uint32_t off = (uint32_t)(s * STAGE) >> 4, a = off + (a_mn ? mn_lo : k_lo), b = off + B_AT + (b_mn ? mn_lo : k_lo);
                         const uint32_t a_step = a_mn ? (2048u >> 4) : (32u >> 4), b_step = b_mn ? (2048u >> 4) : (32u >> 4);     // one 16-deep slice
                         const uint32_t idesc = instr_desc(TM, a_mn, b_mn, 0u, 256u);
@@ -774,11 +843,12 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
             }
         }
         __syncwarp();
-    } else {
+    } else if (warp >= 4) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(MANY_REGS));
         // ---------------- epilogue: warp w has the 32 rows that its tensor-memory quarter holds, and half the columns ----------------
-        const int quarter = warp % 4, half = (warp - 2) / 4;
-        unsigned char* stage_ptr = smem + STAGE_RING + (warp - 2) * 4096;
-        int acc = 0; uint32_t aph = 0;
+        const int quarter = warp % 4, half = (warp - 4) / 4;
+        unsigned char* stage_ptr = smem + STAGE_RING + (warp - 4) * 4096;
+        int acc = 0, e = 0; uint32_t aph = 0, eph = 0;
         bool ok = true;
         const uint32_t mine_tmem = tmem_base + half * NC + ((uint32_t)(quarter * 32) << 16);
         auto release = [&] {
@@ -787,7 +857,11 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
             if (lane == 0) mbar_arrive_remote(tempty_ld + 8 * acc);
             if (++acc == 2) { acc = 0; aph ^= 1; }
         };
-        for (; find_unit(g, w, u); w.unit += pairs) {
+        while (true) {
+            ok = __all_sync(0xffffffffu, mbar_wait(ufull0 + 8 * e, eph, abort_flag));
+            if (!ok) break;
+            const Unit& u = *unit_at(e);
+            if (!u.kblocks) break;
             // no unit of the product before the last reads any more what will be written here
             if (u.op.out >= 0 && u.stage >= 2) {
                 const Class& c = g.c[u.cls];
@@ -828,7 +902,6 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
 #pragma unroll
                 for (int q = 0; q < NC / 16; ++q) tmem_st16(d + q * 16, &v[q * 16]);
                 tmem_st_wait();
-                find_unit(g, w, u);        // (once more, in place of the registers that it would hold across the sums)
             }
             const Class& c = g.c[u.cls];
             const Slot* slot = &c.slot[u.mat];
@@ -873,6 +946,9 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
                     asm volatile("red.relaxed.gpu.global.add.u32 [%0], 1;" ::"l"(&c.slot[u.mat].done) : "memory");
                 }
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(uempty0 + 8 * e);
+            if (++e == UNITS) { e = 0; eph ^= 1; }
         }
     }
 
