@@ -20,6 +20,10 @@ namespace {
 constexpr uint32_t kMuonMagic = 0x0D10B0E5u, kAdamWMagic = 0x0D10ADA3u;
 constexpr int32_t kMaxSteps = 32;
 constexpr size_t kScratchBudget = (size_t)4 << 30;     // per launch
+#ifndef OD_FEW
+#define OD_FEW 24
+#endif
+constexpr int kFewTiles = OD_FEW;
 }  // namespace
 
 struct orthdion_muon_plan {
@@ -81,10 +85,23 @@ Groups group_steps(const orthdion_muon_plan* p) {
     return Groups{p->steps >= 2, p->steps >= 5 && 4 * l >= 5 * s};
 }
 
+// Tiles and square blocks of the products of one matrix, with tiles of CTA pairs or of single CTAs.
+struct Tiles {
+    int32_t sq, x, blocks_sq, blocks_x;
+    int32_t counts() const { return 4 * blocks_sq + 2 * blocks_x; }
+};
+template <class SH>
+Tiles tiles_in(int m, int n) {
+    const int s = std::min(m, n), b = SH::blocks(s);
+    return Tiles{SH::tiles_sym(s), SH::blocks(m) * SH::tiles(n), b * (b + 1) / 2, SH::blocks(m) * SH::blocks(n)};
+}
+Tiles tiles_of(const orthdion_muon_plan* p, bool pair) {
+    return pair ? tiles_in<ns::Shape<true>>((int)p->m, (int)p->n) : tiles_in<ns::Shape<false>>((int)p->m, (int)p->n);
+}
+
 // The scratch of `count` matrices of one plan: byte offsets, strides in elements.
 struct Scratch {
     size_t slot, part, tile_done, x[2], sq[4], bytes;
-    int32_t tiles_sq, tiles_x, counts;
     int64_t x_pitch, x_term, x_mat, s_pitch, s_term, s_mat;
 };
 
@@ -98,11 +115,7 @@ Scratch scratch_layout(const orthdion_muon_plan* p, int count) {
     size_t off = 0;
     c.slot = 0; off += align_up(count * sizeof(ns::Slot), 256);
     c.part = off; off += align_up((size_t)count * ns::MAX_PARTS * 8, 1024);
-    const int64_t st = ns::tiles_along((int)s);
-    c.tiles_sq = (int32_t)(st * (st + 1) / 2);
-    c.tiles_x = ns::tiles_along((int)p->m) * ns::tiles_along((int)p->n);
-    c.counts = 4 * c.tiles_sq + 2 * c.tiles_x;
-    c.tile_done = off; off += align_up((size_t)count * c.counts * 4, 1024);
+    c.tile_done = off; off += align_up((size_t)count * std::max(tiles_of(p, true).counts(), tiles_of(p, false).counts()) * 4, 1024);
     for (int i = 0; i < 2; ++i) {
         c.x[i] = off;
         if (i == 0 || p->steps > 1 + g.pair_first) off += align_up((size_t)count * c.x_mat * 2, 1024);
@@ -126,6 +139,7 @@ struct Launch {
     std::vector<size_t> off;                   // their scratch
     size_t bytes = 0;
     int matrices = 0;
+    bool pair = true;                          // tiles of CTA pairs, or of single CTAs
 };
 
 std::vector<Launch> make_launches(const orthdion_muon_t* hs, int32_t count, size_t* scratch) {
@@ -162,15 +176,20 @@ std::vector<Launch> make_launches(const orthdion_muon_t* hs, int32_t count, size
         }
     }
     *scratch = 0;
-    for (const Launch& l : out) *scratch = std::max(*scratch, l.bytes);
+    for (Launch& l : out) {
+        *scratch = std::max(*scratch, l.bytes);
+        int tiles = 0;             // of the symmetric products, 256 x 256
+        for (const auto& cls : l.classes) tiles += tiles_of(hs[cls[0]], true).sq * (int)cls.size();
+        l.pair = tiles > kFewTiles;
+    }
     return out;
 }
 
 size_t status_bytes(int32_t count) { return align_up((size_t)count * 4, 1024); }
 
-// Maps over the images of a class: (columns, rows, planes, matrices) in boxes of 64 x 128, and (64 columns, rows, groups of 64 columns,
-// planes, matrices) in boxes of two groups of 64 rows.
-void encode(CUtensorMap* k, CUtensorMap* mn, const void* base, int64_t cols, int64_t rows, int terms, int count, int64_t pitch, int64_t term, int64_t mat) {
+// Maps over image i of a class: (columns, rows, planes, matrices) in boxes of 64 columns, and (64 columns, rows, groups of 64 columns, planes,
+// matrices) in boxes of 64 rows; 128 rows or two groups for the first side of a product, as many as one CTA loads of the second.
+void encode(ns::Class& c, int i, bool pair, const void* base, int64_t cols, int64_t rows, int terms, int64_t pitch, int64_t term, int64_t mat) {
     TensorMapEncodeFn enc = tensor_map_encoder();
     if (!enc) { engine_error() = 1; return; }
     const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
@@ -182,17 +201,19 @@ void encode(CUtensorMap* k, CUtensorMap* mn, const void* base, int64_t cols, int
             engine_error() = 2;
         }
     };
-    const cuuint64_t kd[4] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)terms, (cuuint64_t)count};
+    const cuuint64_t kd[4] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)terms, (cuuint64_t)c.count};
     const cuuint64_t ks[3] = {(cuuint64_t)pitch * 2, (cuuint64_t)term * 2, (cuuint64_t)mat * 2};
-    const cuuint32_t kb[4] = {64, 128, (cuuint32_t)terms, 1};
-    map(k, 4, kd, ks, kb);
-    const cuuint64_t md[5] = {64, (cuuint64_t)rows, (cuuint64_t)pitch / 64, (cuuint64_t)terms, (cuuint64_t)count};
+    const cuuint64_t md[5] = {64, (cuuint64_t)rows, (cuuint64_t)pitch / 64, (cuuint64_t)terms, (cuuint64_t)c.count};
     const cuuint64_t ms[4] = {(cuuint64_t)pitch * 2, 128, (cuuint64_t)term * 2, (cuuint64_t)mat * 2};
-    const cuuint32_t mb[5] = {64, 64, 2, (cuuint32_t)terms, 1};
-    map(mn, 5, md, ms, mb);
+    for (int side = 0; side < 2; ++side) {
+        const cuuint32_t n = side == 0 || pair ? 128 : 64;
+        const cuuint32_t kb[4] = {64, n, (cuuint32_t)terms, 1}, mb[5] = {64, 64, n / 64, (cuuint32_t)terms, 1};
+        map(side ? &c.k_b[i] : &c.k_a[i], 4, kd, ks, kb);
+        map(side ? &c.mn_b[i] : &c.mn_a[i], 5, md, ms, mb);
+    }
 }
 
-int g_pairs[kMaxDevices] = {};       // CTA pairs of the chain kernel that the device runs at once; written under ensure_attributes()'s lock
+int g_at_once[kMaxDevices][2] = {};       // single CTAs and CTA pairs of the chain kernel that the device runs at once; written under ensure_attributes()'s lock
 
 int current_device() {
     int dev = -1;
@@ -204,7 +225,7 @@ void run_launch(const orthdion_muon_t* hs, const Launch& l, void* const* X, floa
                 char* scratch, cudaStream_t st) {
     std::unique_ptr<ns::ChainArgs> args(new ns::ChainArgs());
     ns::Table all{};
-    const int terms = terms_of(hs[l.classes[0][0]]), pairs = g_pairs[current_device()];
+    const int terms = terms_of(hs[l.classes[0][0]]), at_once = g_at_once[current_device()][l.pair];
     args->classes = (int32_t)l.classes.size();
     for (size_t k = 0; k < l.classes.size(); ++k) {
         const std::vector<int>& idx = l.classes[k];
@@ -230,13 +251,14 @@ void run_launch(const orthdion_muon_t* hs, const Launch& l, void* const* X, floa
         const int64_t s = std::min(p->m, p->n);
         for (int i = 0; i < 2; ++i) {
             c.x[i] = reinterpret_cast<__half*>(base + sc.x[i]);
-            encode(&c.k_x[i], &c.mn_x[i], c.x[i], p->n, p->m, terms, c.count, sc.x_pitch, sc.x_term, sc.x_mat);
+            encode(c, 4 + i, l.pair, c.x[i], p->n, p->m, terms, sc.x_pitch, sc.x_term, sc.x_mat);
         }
         for (int i = 0; i < 4; ++i) {
             c.sq[i] = reinterpret_cast<__half*>(base + sc.sq[i]);
-            encode(&c.k_sq[i], &c.mn_sq[i], c.sq[i], s, s, terms, c.count, sc.s_pitch, sc.s_term, sc.s_mat);
+            encode(c, i, l.pair, c.sq[i], s, s, terms, sc.s_pitch, sc.s_term, sc.s_mat);
         }
-        c.tiles_sq = sc.tiles_sq; c.tiles_x = sc.tiles_x; c.counts = sc.counts;
+        const Tiles tl = tiles_of(p, l.pair);
+        c.tiles_sq = tl.sq; c.tiles_x = tl.x; c.blocks_sq = tl.blocks_sq; c.blocks_x = tl.blocks_x; c.counts = tl.counts();
         c.tile_done = reinterpret_cast<uint32_t*>(base + sc.tile_done);
         c.update = update;
         c.x_bf16 = p->x_dtype == ORTHDION_DTYPE_BF16;
@@ -270,19 +292,21 @@ void run_launch(const orthdion_muon_t* hs, const Launch& l, void* const* X, floa
     int units = 0;                 // of the products with the most tiles
     for (int k = 0; k < args->classes; ++k) units += std::max(args->c[k].tiles_sq, args->c[k].tiles_x) * args->c[k].count;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(2 * std::min(pairs, units)));
+    cfg.gridDim = dim3((unsigned)((l.pair ? 2 : 1) * std::min(at_once, units)));
     cfg.blockDim = dim3(ns::THREADS);
     cfg.dynamicSmemBytes = ns::SMEM_BYTES;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[0].val.clusterDim.x = l.pair ? 2 : 1; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     // (pairs wait for one another's tiles: all of them run at once, or none)
     attr[1].id = cudaLaunchAttributeCooperative;
     attr[1].val.cooperative = 1;
     cfg.attrs = attr; cfg.numAttrs = 2;
     prof::Scope scope(prof::S_NS_PRODUCT, st);
-    const cudaError_t e = terms == 2 ? cudaLaunchKernelEx(&cfg, ns::chain_kernel<2>, all, *args) : cudaLaunchKernelEx(&cfg, ns::chain_kernel<1>, all, *args);
+    const auto kernel = l.pair ? (terms == 2 ? ns::chain_kernel<true, 2> : ns::chain_kernel<true, 1>)
+                               : (terms == 2 ? ns::chain_kernel<false, 2> : ns::chain_kernel<false, 1>);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, all, *args);
     if (e != cudaSuccess) engine_error() = LAUNCH_FAILED;
 }
 
@@ -294,22 +318,24 @@ int ensure_attributes() {
     std::lock_guard<std::mutex> lock(mu);
     if (state[dev]) return state[dev] > 0 ? 0 : ORTHDION_ERR_CUDA;
     cudaError_t e = cudaSuccess;
-    auto set = [&](auto* kernel) {
+    auto set = [&](auto* kernel, bool pair) {
         if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ns::SMEM_BYTES);
         cudaLaunchConfig_t cfg{};
         cfg.gridDim = dim3((unsigned)(sm_count() / 2 * 2)); cfg.blockDim = dim3(ns::THREADS);
         cfg.dynamicSmemBytes = ns::SMEM_BYTES;
         cudaLaunchAttribute attr[1];
         attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        attr[0].val.clusterDim.x = pair ? 2 : 1; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
         cfg.attrs = attr; cfg.numAttrs = 1;
         int n = 0;
         if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
         if (e == cudaSuccess && n < 1) e = cudaErrorInvalidConfiguration;
-        g_pairs[dev] = g_pairs[dev] ? std::min(g_pairs[dev], n) : n;
+        g_at_once[dev][pair] = g_at_once[dev][pair] ? std::min(g_at_once[dev][pair], n) : n;
     };
-    set(ns::chain_kernel<1>);
-    set(ns::chain_kernel<2>);
+    set(ns::chain_kernel<true, 1>, true);
+    set(ns::chain_kernel<true, 2>, true);
+    set(ns::chain_kernel<false, 1>, false);
+    set(ns::chain_kernel<false, 2>, false);
     if (e != cudaSuccess) std::fprintf(stderr, "orthdion: kernel attribute setup failed on device %d: %s\n", dev, cudaGetErrorString(e));
     state[dev] = e == cudaSuccess ? 1 : -1;
     return e == cudaSuccess ? 0 : ORTHDION_ERR_CUDA;

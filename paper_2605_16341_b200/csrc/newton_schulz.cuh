@@ -254,36 +254,52 @@ constexpr int STAGE_RING = 196608;            // bytes of the operand ring
 // gives back: 128 x 80 + 256 x 208 of the 384 x 168 that the block is launched with.
 constexpr int THREADS = 384, FEW_REGS = 80, MANY_REGS = 208;
 static_assert(128 * FEW_REGS + 256 * MANY_REGS <= THREADS * 168, "registers");
-constexpr int MAX_STAGES = 6;
+constexpr int MAX_STAGES = 8;
 constexpr int UNITS = 4;                      // that the scout is ahead of the epilogue at most
 constexpr int SMEM_BYTES = 1024 + STAGE_RING + 8 * 4096 + 256 + UNITS * 128;      // operands, epilogue blocks, barriers, units
-constexpr int TM = 256;                       // rows (128 of each CTA of a pair) and columns of a tile
-constexpr int NC = TM / 2;                    // columns of an epilogue warp
+// Two shapes of a tile.  PAIR: 256 x 256, two CTAs of 128 rows and 128 columns' operands each: 32 KB of operands (a plane) for 512 cycles of
+// MMAs, about what a multiprocessor takes in.  Else 128 x 64 of one CTA, 24 KB for 128 cycles: for calls of few tiles, whose
+// products then run on six times as many multiprocessors, and whose tiles leave six times as fast.
+template <bool PAIR>
+struct Shape {
+    static constexpr int ROWS = PAIR ? 256 : 128, COLS = PAIR ? 256 : 64, Q = ROWS / COLS;
+    static constexpr int DEPTH = ROWS / 64;                 // depth blocks of a square block of an image, at whose granularity tiles are waited for
+    static constexpr int CTAS = PAIR ? 2 : 1;
+    static constexpr int B_ROWS = PAIR ? 128 : 64;          // of B that one CTA loads
+    static constexpr int NC = COLS / 2;                     // columns of an epilogue warp
+    static constexpr int ARRIVALS = 8 * CTAS;               // at a count for one tile: the epilogue warps
+    __host__ __device__ static constexpr int blocks(int n) { return (n + ROWS - 1) / ROWS; }
+    __host__ __device__ static constexpr int tiles(int n) { return (n + COLS - 1) / COLS; }
+    // tiles of a symmetric image in the block rows before i; of n rows in all; and of one of the square blocks of n columns
+    __host__ __device__ static constexpr int before(int i) { return Q * (i * (i + 1) / 2); }
+    __host__ __device__ static constexpr int tiles_sym(int n) { return before(blocks(n)) - (Q * blocks(n) - tiles(n)); }
+    __host__ __device__ static constexpr int width(int block, int n) { return tiles(n) - Q * block < Q ? tiles(n) - Q * block : Q; }
+};
 constexpr int GROUP_ROWS = 8;                 // tile rows that are walked together, column by column
-constexpr int ARRIVALS = 16;                  // at a count for one unit: the epilogue warps of a pair
-constexpr int MAX_CLASSES = 8;
+constexpr int MAX_CLASSES = 6;                // (their maps and the rest come to 24 KB of kernel parameters)
 constexpr int MAX_ITER = 32;                  // steps of a schedule
 
 // Matrices of one plan.
 struct Class {
-    // Boxes over an image, all planes of one matrix: 64 columns of 128 rows, an operand tile along rows (K-major); and two groups of
-    // 64 columns of 64 rows, one along columns (MN-major; what lies between the last column and the pitch only reaches results beyond the edge).
-    alignas(64) CUtensorMap k_x[2];
-    CUtensorMap k_sq[4], mn_x[2], mn_sq[4];
+    // Boxes over image i (0 to 3: sq, 4 and 5: X), all planes of one matrix, for either side of a product: 64 columns of 128 or 64 rows, an operand
+    // tile along rows (K-major); and two or one groups of 64 columns of 64 rows, one along columns (MN-major; what lies between the last column
+    // and the pitch only reaches results beyond the edge).
+    alignas(64) CUtensorMap k_a[6];
+    CUtensorMap k_b[6], mn_a[6], mn_b[6];
     __half* x[2];
     __half* sq[4];
     int64_t x_pitch, x_term, x_mat, s_pitch, s_term, s_mat;     // in elements
     Slot* slot;
-    uint32_t* tile_done;                      // counts of the tiles of sq[0] to sq[3] (row by row below the diagonal) and of X
+    uint32_t* tile_done;                      // counts of the square blocks of sq[0] to sq[3] (row by row below the diagonal) and of X
     int64_t ld_x;
     int32_t m, n, count, first;               // first: its first matrix in the table
     int32_t steps, pair_first, pair_last;     // steps of the iteration; whether the first and the last two of them are one group
-    int32_t tiles_sq, tiles_x, counts;        // tiles of one s x s product, of one product with X; counts of one matrix
+    int32_t tiles_sq, tiles_x;                // tiles of one s x s product, of one product with X
+    int32_t blocks_sq, blocks_x, counts;      // square blocks of those; counts of one matrix
     int32_t update, x_bf16, x_vec;
     float wc, wd;
     float abc[MAX_ITER][3];
 };
-__host__ __device__ constexpr int tiles_along(int n) { return (n + TM - 1) / TM; }
 struct ChainArgs {
     int32_t classes, stages;                  // stages: most products of a class
     Class c[MAX_CLASSES];
@@ -349,6 +365,7 @@ struct Unit {
     const CUtensorMap *k_a, *k_b, *mn_a, *mn_b;
 };
 // Makes w.unit a unit of (w.stage, w.cls), or returns false behind the last.
+template <class SH>
 __device__ __forceinline__ bool find_unit(const ChainArgs& g, Walk& w, Unit& u) {
     while (true) {
         if (w.stage >= g.stages) return false;
@@ -372,12 +389,12 @@ __device__ __forceinline__ bool find_unit(const ChainArgs& g, Walk& w, Unit& u) 
     u.rows = apply ? c.m : s; u.cols = apply ? c.n : s;
     u.kblocks = ((u.op.kind == OP_GRAM ? l : s) + 63) / 64;
     if (!apply) {
-        u.ti = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
-        while (u.ti * (u.ti + 1) / 2 > t) --u.ti;
-        while ((u.ti + 1) * (u.ti + 2) / 2 <= t) ++u.ti;
-        u.tj = t - u.ti * (u.ti + 1) / 2;
+        u.ti = (int)((sqrtf((8.f / SH::Q) * t + 1.f) - 1.f) * 0.5f);
+        while (SH::before(u.ti) > t) --u.ti;
+        while (SH::before(u.ti + 1) <= t) ++u.ti;
+        u.tj = t - SH::before(u.ti);
     } else {
-        const int n_tiles = tiles_along(u.cols), m_tiles = tiles_along(u.rows);
+        const int n_tiles = SH::tiles(u.cols), m_tiles = SH::blocks(u.rows);
         const int per = GROUP_ROWS * n_tiles, grp = t / per, first = grp * GROUP_ROWS, high = min(GROUP_ROWS, m_tiles - first), in = t - grp * per;
         u.tj = in / high;
         u.ti = first + in - u.tj * high;
@@ -392,16 +409,28 @@ template <class T> __device__ __forceinline__ T from_float(float v) {
     else return v;
 }
 
-// The box of a map at (column, row) or (row, 64-column group) of one matrix, for a CTA of a pair: counted on the leader's mbarrier.
+// The box of a map at (column, row) or (row, 64-column group) of one matrix; PAIR: for a CTA of a pair, counted on the leader's mbarrier.
+template <bool PAIR>
 __device__ __forceinline__ void tma_load_k(uint32_t dst, const CUtensorMap* map, int col, int row, int mat, uint32_t bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
-        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(col), "r"(row), "r"(0), "r"(mat), "r"(bar) : "memory");
+    if (PAIR)
+        asm volatile(
+            "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+            ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(col), "r"(row), "r"(0), "r"(mat), "r"(bar) : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+            ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(col), "r"(row), "r"(0), "r"(mat), "r"(bar) : "memory");
 }
+template <bool PAIR>
 __device__ __forceinline__ void tma_load_mn(uint32_t dst, const CUtensorMap* map, int row, int group, int mat, uint32_t bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
-        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(group), "r"(0), "r"(mat), "r"(bar) : "memory");
+    if (PAIR)
+        asm volatile(
+            "cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+            ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(group), "r"(0), "r"(mat), "r"(bar) : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+            ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(group), "r"(0), "r"(mat), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* v) {
     asm volatile(
@@ -421,30 +450,35 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const float* v) {
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// One side of a product: an image, read along the unit's rows (or columns) `tile`.
+// One side of a product: an image, read along its rows (or columns) of a square block.
 struct Side {
-    int image, tile;
+    int image, block;
     bool sym;              // a symmetric image: mirrored above the diagonal
     bool mn;               // X along its columns: depth runs down its rows
-    // index of the tile of depth block kb in its image's counts
-    __device__ __forceinline__ int place(const Class& c, int kb) const {
-        const int k = kb / 4;
-        if (sym) {
-            const int hi = max(k, tile), lo = min(k, tile);
-            return image * c.tiles_sq + hi * (hi + 1) / 2 + lo;
-        }
-        const int row = mn ? k : tile, col = mn ? tile : k;
-        return 4 * c.tiles_sq + (image - 4) * c.tiles_x + row * tiles_along(c.n) + col;
-    }
 };
+// Where the count of depth block kb stands, and what one write of it adds.
+template <class SH>
+__device__ __forceinline__ int place_of(const Class& c, const Side& d, int kb, int& arrivals) {
+    const int k = kb / SH::DEPTH;
+    if (d.sym) {
+        const int hi = max(k, d.block), lo = min(k, d.block);
+        arrivals = SH::ARRIVALS * SH::width(lo, min(c.m, c.n));
+        return d.image * c.blocks_sq + hi * (hi + 1) / 2 + lo;
+    }
+    const int row = d.mn ? k : d.block, col = d.mn ? d.block : k;
+    arrivals = SH::ARRIVALS * SH::width(col, c.n);
+    return 4 * c.blocks_sq + (d.image - 4) * c.blocks_x + row * SH::blocks(c.n) + col;
+}
+template <class SH>
 __device__ __forceinline__ void sides_of(const Class& c, const Unit& u, Side& a, Side& b) {
     const bool wide = c.m <= c.n, gram_tall = u.op.kind == OP_GRAM && !wide;
-    a = Side{u.op.a, u.ti, u.op.a < 4, gram_tall};
-    b = Side{u.op.b, u.tj, u.op.b < 4, gram_tall || (u.op.kind == OP_APPLY && wide)};
+    const int ia = u.ti, ib = u.tj / SH::Q;
+    a = Side{u.op.a, ia, u.op.a < 4, gram_tall};
+    b = Side{u.op.b, ib, u.op.b < 4, gram_tall || (u.op.kind == OP_APPLY && wide)};
     // X is the second side of a product with a wide matrix, the first with a tall one
     if (u.op.kind == OP_APPLY && !wide) {
-        a = Side{u.op.b, u.ti, false, false};
-        b = Side{u.op.a, u.tj, true, false};
+        a = Side{u.op.b, ia, false, false};
+        b = Side{u.op.a, ib, true, false};
     }
 }
 
@@ -485,10 +519,11 @@ struct Out {
     int64_t pitch, term;
     int rows, cols;
     float beta, diag;
+    bool mirror;                 // also to the mirrored place
 };
-template <int TERMS>
+template <int TERMS, int NC>
 __device__ __forceinline__ void image_epilogue(const Out& g, uint32_t d, float alpha, int row_w, int lane, int col_w, unsigned char* stage_ptr) {
-    constexpr int W = 64 / TERMS, CH = W / 8, RPI = 32 / CH, IT = 32 / RPI;      // chunks of 16 bytes a row, rows a turn, turns
+    constexpr int W = 64 / TERMS < NC ? 64 / TERMS : NC, CH = W / 8, RPI = 32 / CH, IT = 32 / RPI;      // chunks of 16 bytes a row, rows a turn, turns
     const int sr = lane / CH, sc = lane % CH;                // (sr, sc): row and chunk that this lane moves
     auto at = [](int t, int r, int ch) { return t * 2048 + r * (2 * W) + ((CH == 8 ? ch ^ (r & 7) : ch ^ ((r >> 1) & 3)) << 4); };
     const int64_t lane_at = (int64_t)(row_w + sr) * g.pitch + col_w + sc * 8;
@@ -570,6 +605,20 @@ __device__ __forceinline__ void image_epilogue(const Out& g, uint32_t d, float a
                         *reinterpret_cast<uint4*>(g.img + t * g.term + lane_at + RPI * i * g.pitch + q * W) =
                             *reinterpret_cast<const uint4*>(stage_ptr + at(t, sr + RPI * i, sc));
         }
+        if (g.mirror) {
+#pragma unroll 1
+            for (int i = lane; i < TERMS * W * 4; i += 32) {               // eight rows of one column of one plane
+                const int t = i / (W * 4), e = i / 4 % W, r0 = i % 4 * 8;
+                if (col + e < g.cols && row_w + r0 < g.rows) {
+                    uint32_t h[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        h[k] = *reinterpret_cast<const uint16_t*>(stage_ptr + at(t, r0 + 2 * k, e / 8) + e % 8 * 2) |
+                               (uint32_t)*reinterpret_cast<const uint16_t*>(stage_ptr + at(t, r0 + 2 * k + 1, e / 8) + e % 8 * 2) << 16;
+                    *reinterpret_cast<uint4*>(g.img + t * g.term + (int64_t)(col + e) * g.pitch + row_w + r0) = make_uint4(h[0], h[1], h[2], h[3]);
+                }
+            }
+        }
         __syncwarp();
     }
 }
@@ -581,7 +630,7 @@ struct Final {
     int rows, cols, update, x_vec;       // X <- wc X - wd D, or X <- D; x_vec: rows of X on 16-byte boundaries, and whole vectors
     float wc, wd;
 };
-template <class T>
+template <class T, int NC>
 __device__ __forceinline__ void final_epilogue(const Final& g, uint32_t d, float alpha, int row_w, int lane, int col_w, unsigned char* stage_ptr) {
     void* X = g.X;
     float* blk = reinterpret_cast<float*>(stage_ptr);
@@ -657,11 +706,14 @@ __device__ __forceinline__ void final_epilogue(const Final& g, uint32_t d, float
     }
 }
 
-template <int TERMS>
+template <bool PAIR, int TERMS>
 __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant__ Table table, const __grid_constant__ ChainArgs g) {
-    constexpr int A_BYTES = 128 * 128 * TERMS, STAGE = 2 * A_BYTES, NS = STAGE_RING / STAGE;
-    const int crank = (int)cluster_ctarank();
-    const int pair0 = (int)(blockIdx.x >> 1), pairs = (int)(gridDim.x >> 1);
+    using SH = Shape<PAIR>;
+    constexpr int NC = SH::NC;
+    constexpr int A_BYTES = 128 * 128 * TERMS, STAGE = A_BYTES + SH::B_ROWS * 128 * TERMS, NS = STAGE_RING / STAGE;
+    static_assert(NS <= MAX_STAGES, "barriers");
+    const int crank = PAIR ? (int)cluster_ctarank() : 0;
+    const int pair0 = (int)blockIdx.x / SH::CTAS, pairs = (int)gridDim.x / SH::CTAS;
 
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
@@ -675,22 +727,25 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < NS; ++s) { mbar_init(full0 + 8 * s, 2); mbar_init(empty0 + 8 * s, 1); }
-        for (int a = 0; a < 2; ++a) { mbar_init(tfull0 + 8 * a, 1); mbar_init(tempty0 + 8 * a, 2 * 8); }
+        for (int s = 0; s < NS; ++s) { mbar_init(full0 + 8 * s, SH::CTAS); mbar_init(empty0 + 8 * s, 1); }
+        for (int a = 0; a < 2; ++a) { mbar_init(tfull0 + 8 * a, 1); mbar_init(tempty0 + 8 * a, SH::ARRIVALS); }
         for (int e = 0; e < UNITS; ++e) { mbar_init(ufull0 + 8 * e, 1); mbar_init(uempty0 + 8 * e, 8); }
         tmem_slot[2] = 0;
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_smem();
     }
-    if (warp == 1) tmem_alloc_pair(smem_u32(tmem_slot), 2 * TM);
+    if (warp == 1) {
+        if (PAIR) tmem_alloc_pair(smem_u32(tmem_slot), 2 * SH::COLS);
+        else tmem_alloc(smem_u32(tmem_slot), 2 * SH::COLS);
+    }
     tc_fence_before();
     __syncthreads();
-    cluster_sync_all();                 // the peer's barriers are initialised before anything reaches them
+    if (PAIR) cluster_sync_all();       // the peer's barriers are initialised before anything reaches them
     tc_fence_after();
     grid_dependency();
     const uint32_t tmem_base = *tmem_slot;
-    const uint32_t full_ld = map_to_rank(full0, 0), tempty_ld = map_to_rank(tempty0, 0);
+    const uint32_t full_ld = PAIR ? map_to_rank(full0, 0) : full0, tempty_ld = PAIR ? map_to_rank(tempty0, 0) : tempty0;
     // The scout's units, each until the epilogue warps are through with it; and how many depth blocks of all units so far it has found there.
     Unit* ring = reinterpret_cast<Unit*>(smem + STAGE_RING + 8 * 4096 + 256);
     static_assert(sizeof(Unit) <= 128, "units in shared memory");
@@ -709,18 +764,16 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
             Unit& u = *unit_at(e);
             int more = 0;
             if (lane == 0) {
-                more = find_unit(g, w, u);
+                more = find_unit<SH>(g, w, u);
                 w.unit += pairs;
                 if (more) {
                     const Class& c = g.c[u.cls];
                     Side a, b;
-                    sides_of(c, u, a, b);
-                    u.a_turn = a.sym ? 4 * (a.tile + 1) : a.mn ? 0 : u.kblocks;
-                    u.b_turn = b.sym ? 4 * (b.tile + 1) : b.mn ? 0 : u.kblocks;
-                    u.k_a = a.image < 4 ? &c.k_sq[a.image] : &c.k_x[a.image - 4];
-                    u.k_b = b.image < 4 ? &c.k_sq[b.image] : &c.k_x[b.image - 4];
-                    u.mn_a = a.image < 4 ? &c.mn_sq[a.image] : &c.mn_x[a.image - 4];
-                    u.mn_b = b.image < 4 ? &c.mn_sq[b.image] : &c.mn_x[b.image - 4];
+                    sides_of<SH>(c, u, a, b);
+                    u.a_turn = a.sym ? SH::DEPTH * (a.block + 1) : a.mn ? 0 : u.kblocks;
+                    u.b_turn = b.sym ? SH::DEPTH * (b.block + 1) : b.mn ? 0 : u.kblocks;
+                    u.k_a = &c.k_a[a.image]; u.mn_a = &c.mn_a[a.image];
+                    u.k_b = &c.k_b[b.image]; u.mn_b = &c.mn_b[b.image];
                 } else {
                     u.kblocks = 0;                 // the end
                 }
@@ -730,17 +783,19 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
             if (!more) break;
             const Class& c = g.c[u.cls];
             Side a, b;
-            sides_of(c, u, a, b);
+            sides_of<SH>(c, u, a, b);
             const uint32_t* counts = c.tile_done + (int64_t)u.mat * c.counts;
-            const uint32_t want_a = ARRIVALS * writes_of(c, u.op, a.image), want_b = ARRIVALS * writes_of(c, u.op, b.image);
+            const uint32_t writes_a = writes_of(c, u.op, a.image), writes_b = writes_of(c, u.op, b.image);
             const int kblocks = u.kblocks;
             const long long t0 = clock64();
             for (int kb = 0, spins = 0; kb < kblocks; ++spins) {
-                const int k = kb + 4 * lane;
+                const int k = kb + SH::DEPTH * lane;
                 bool there = true;
                 if (k < kblocks) {
-                    const uint32_t x = load_relaxed(counts + a.place(c, k)), y = load_relaxed(counts + b.place(c, k));
-                    there = (int32_t)(x - want_a) >= 0 && (int32_t)(y - want_b) >= 0;
+                    int per_a, per_b;
+                    const int at_a = place_of<SH>(c, a, k, per_a), at_b = place_of<SH>(c, b, k, per_b);
+                    const uint32_t x = load_relaxed(counts + at_a), y = load_relaxed(counts + at_b);
+                    there = (int32_t)(x - writes_a * per_a) >= 0 && (int32_t)(y - writes_b * per_b) >= 0;
                 }
                 const uint32_t missing = __ballot_sync(0xffffffffu, !there);
                 const int tiles = missing ? __ffs(missing) - 1 : 32;
@@ -748,7 +803,7 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
                     asm volatile("fence.acq_rel.gpu;" ::: "memory");
                     asm volatile("fence.proxy.async;" ::: "memory");
                     __syncwarp();
-                    kb = min(kblocks, kb + 4 * tiles);
+                    kb = min(kblocks, kb + SH::DEPTH * tiles);
                     if (lane == 0) asm volatile("st.release.cta.shared::cta.u32 [%0], %1;" ::"r"(ready_at), "r"(total + kb) : "memory");
                 } else {
                     if ((spins & 15) == 15 && (*abort_flag || clock64() - t0 > WAIT_LIMIT_CYCLES)) { *abort_flag = 1; ok = false; }
@@ -771,7 +826,7 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
                 const int kblocks = u.kblocks, mat = u.mat, a_turn = u.a_turn, b_turn = u.b_turn;
                 if (!kblocks) break;
                 const CUtensorMap *ka = u.k_a, *kb_ = u.k_b, *ma = u.mn_a, *mb = u.mn_b;
-                const int ar = u.ti * TM + crank * 128, br = u.tj * TM + crank * 128;
+                const int ar = u.ti * SH::ROWS + crank * 128, br = u.tj * SH::COLS + crank * SH::B_ROWS;
                 for (int kb = 0; kb < kblocks && ok;) {
                     const long long t0 = clock64();
                     for (int spins = 0; ready <= total + kb; ++spins) {
@@ -787,11 +842,12 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
                     for (; kb < end; ++kb) {
                         if (!mbar_wait(empty0 + 8 * s, ph ^ 1, abort_flag)) { ok = false; break; }
                         const uint32_t fb = full_ld + 8 * s, dst = base + s * STAGE;
-                        mbar_arrive_expect_tx_remote(fb, STAGE);
-                        if (a_mn) tma_load_mn(dst, ma, kb * 64, ar / 64, mat, fb);
-                        else tma_load_k(dst, ka, kb * 64, ar, mat, fb);
-                        if (b_mn) tma_load_mn(dst + A_BYTES, mb, kb * 64, br / 64, mat, fb);
-                        else tma_load_k(dst + A_BYTES, kb_, kb * 64, br, mat, fb);
+                        if (PAIR) mbar_arrive_expect_tx_remote(fb, STAGE);
+                        else mbar_arrive_expect_tx(fb, STAGE);
+                        if (a_mn) tma_load_mn<PAIR>(dst, ma, kb * 64, ar / 64, mat, fb);
+                        else tma_load_k<PAIR>(dst, ka, kb * 64, ar, mat, fb);
+                        if (b_mn) tma_load_mn<PAIR>(dst + A_BYTES, mb, kb * 64, br / 64, mat, fb);
+                        else tma_load_k<PAIR>(dst + A_BYTES, kb_, kb * 64, br, mat, fb);
                         if (++s == NS) { s = 0; ph ^= 1; }
                     }
                 }
@@ -807,7 +863,7 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
             const uint64_t k_desc = smem_desc(0, 16, 1024), mn_desc = smem_desc(0, 8192, 1024);
             const uint32_t d_hi = (uint32_t)(k_desc >> 32);             // (both forms')
             const uint32_t k_lo = (uint32_t)k_desc + (base >> 4), mn_lo = (uint32_t)mn_desc + (base >> 4);
-            constexpr uint32_t TERM = 16384u >> 4, B_AT = (uint32_t)A_BYTES >> 4;
+            constexpr uint32_t A_TERM = 16384u >> 4, B_TERM = (uint32_t)(SH::B_ROWS * 128) >> 4, B_AT = (uint32_t)A_BYTES >> 4;
             int s = 0, acc = 0, e = 0; uint32_t ph = 0, aph = 0, eph = 0;
             bool ok = true;
             while (ok && mbar_wait(ufull0 + 8 * e, eph, abort_flag)) {
@@ -818,26 +874,26 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
                 for (int k0 = 0; k0 < kblocks && ok; k0 += chunk) {
                     if (!mbar_wait(tempty0 + 8 * acc, aph ^ 1, abort_flag)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t d = tmem_base + acc * TM;
+                    const uint32_t d = tmem_base + acc * SH::COLS;
                     for (int kb = k0; kb < k0 + chunk; ++kb) {
                         if (!mbar_wait(full0 + 8 * s, ph, abort_flag)) { ok = false; break; }
                         const bool a_mn = kb >= a_turn, b_mn = kb >= b_turn;
                         const uint32_t off = (uint32_t)(s * STAGE) >> 4, a = off + (a_mn ? mn_lo : k_lo), b = off + B_AT + (b_mn ? mn_lo : k_lo);
                         const uint32_t a_step = a_mn ? (2048u >> 4) : (32u >> 4), b_step = b_mn ? (2048u >> 4) : (32u >> 4);     // one 16-deep slice
-                        const uint32_t idesc = instr_desc(TM, a_mn, b_mn, 0u, 256u);
+                        const uint32_t idesc = instr_desc(SH::COLS, a_mn, b_mn, 0u, PAIR ? 256u : 128u);
                         if (TERMS == 2) {
                             // the small products first: an addition truncates at the accumulator's size of the moment
-                            umma_slices<true, 4, false>(d, a, d_hi, b + TERM, d_hi, a_step, b_step, 0, 0, idesc, 0u);
-                            umma_slices<true, 4, false>(d, a + TERM, d_hi, b, d_hi, a_step, b_step, 0, 0, idesc, 1u);
-                            umma_slices<true, 4, false>(d, a, d_hi, b, d_hi, a_step, b_step, 0, 0, idesc, 1u);
+                            umma_slices<PAIR, 4, false>(d, a, d_hi, b + B_TERM, d_hi, a_step, b_step, 0, 0, idesc, 0u);
+                            umma_slices<PAIR, 4, false>(d, a + A_TERM, d_hi, b, d_hi, a_step, b_step, 0, 0, idesc, 1u);
+                            umma_slices<PAIR, 4, false>(d, a, d_hi, b, d_hi, a_step, b_step, 0, 0, idesc, 1u);
                         } else {
-                            umma_slices<true, 4, false>(d, a, d_hi, b, d_hi, a_step, b_step, 0, 0, idesc, kb > k0 ? 1u : 0u);
+                            umma_slices<PAIR, 4, false>(d, a, d_hi, b, d_hi, a_step, b_step, 0, 0, idesc, kb > k0 ? 1u : 0u);
                         }
-                        commit_any<true>(empty0 + 8 * s);
+                        commit_any<PAIR>(empty0 + 8 * s);
                         if (++s == NS) { s = 0; ph ^= 1; }
                     }
                     if (!ok) break;
-                    commit_any<true>(tfull0 + 8 * acc);
+                    commit_any<PAIR>(tfull0 + 8 * acc);
                     if (++acc == 2) { acc = 0; aph ^= 1; }
                 }
             }
@@ -854,7 +910,7 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
         auto release = [&] {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive_remote(tempty_ld + 8 * acc);
+            if (lane == 0) { if (PAIR) mbar_arrive_remote(tempty_ld + 8 * acc); else mbar_arrive(tempty0 + 8 * acc); }
             if (++acc == 2) { acc = 0; aph ^= 1; }
         };
         while (true) {
@@ -865,7 +921,7 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
             // no unit of the product before the last reads any more what will be written here
             if (u.op.out >= 0 && u.stage >= 2) {
                 const Class& c = g.c[u.cls];
-                const uint32_t want = ARRIVALS * units_before(c, u.stage - 1, op_of(c, u.stage - 1).group);
+                const uint32_t want = SH::ARRIVALS * units_before(c, u.stage - 1, op_of(c, u.stage - 1).group);
                 ok = __all_sync(0xffffffffu, wait_count(&c.slot[u.mat].done, want, abort_flag));
                 if (!ok) break;
             }
@@ -885,7 +941,7 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
                     ok = __all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * acc, aph, abort_flag));
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t d = mine_tmem + acc * TM;
+                    const uint32_t d = mine_tmem + acc * SH::COLS;
 #pragma unroll
                     for (int q = 0; q < NC / 16; ++q) {
                         uint32_t x[16];
@@ -898,17 +954,20 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
                     release();
                 }
                 if (!ok) break;
-                const uint32_t d = mine_tmem + acc * TM;
+                const uint32_t d = mine_tmem + acc * SH::COLS;
 #pragma unroll
                 for (int q = 0; q < NC / 16; ++q) tmem_st16(d + q * 16, &v[q * 16]);
                 tmem_st_wait();
             }
             const Class& c = g.c[u.cls];
             const Slot* slot = &c.slot[u.mat];
-            const int row_w = u.ti * TM + crank * 128 + quarter * 32, col_w = u.tj * TM + half * NC;
-            const uint32_t d = mine_tmem + acc * TM;
+            const int row_w = u.ti * SH::ROWS + crank * 128 + quarter * 32, col_w = u.tj * SH::COLS + half * NC;
+            const uint32_t d = mine_tmem + acc * SH::COLS;
             const bool apply = u.op.kind == OP_APPLY;
-            if (row_w < u.rows && col_w < u.cols) {
+            // In a 256 x 256 tile on the diagonal the 128 x 128 block above it is the one below, mirrored, as it is between tiles of the other
+            // shape: Q A rounds another way above the diagonal than below, and a matrix gets the same bits in whatever call it stands.
+            const bool on_diagonal = PAIR && !apply && u.ti == u.tj, above = on_diagonal && crank == 0 && half == 1;
+            if (row_w < u.rows && col_w < u.cols && !above) {
                 float alpha = 1.f / UNIT;
                 // the images hold UNIT times the value, the first one of X divided by sigma
                 if (u.op.group == 0 && u.op.kind == OP_GRAM) { const float sg = __ldcg(&slot->sigma); alpha *= sg * sg; }
@@ -919,6 +978,7 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
                     o.img = (apply ? c.x[u.op.out - 4] : c.sq[u.op.out]) + at;
                     o.pitch = apply ? c.x_pitch : c.s_pitch; o.term = apply ? c.x_term : c.s_term;
                     o.rows = u.rows; o.cols = u.cols;
+                    o.mirror = on_diagonal && crank == 1 && half == 0;
                     o.add = nullptr;
                     if (u.op.kind == OP_POLY) {
                         const float* k = c.abc[u.op.step];
@@ -926,11 +986,11 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
                         o.beta = k[1]; o.diag = k[0] * UNIT;
                         o.add = c.sq[u.op.a] + at;
                     }
-                    image_epilogue<TERMS>(o, d, alpha, row_w, lane, col_w, stage_ptr);
+                    image_epilogue<TERMS, NC>(o, d, alpha, row_w, lane, col_w, stage_ptr);
                 } else if (!__ldcg(&slot->status)) {
                     const Final f{table.w[c.first + u.mat].X, c.ld_x, u.rows, u.cols, c.update, c.x_vec, c.wc, c.wd};
-                    if (c.x_bf16) final_epilogue<__nv_bfloat16>(f, d, alpha / UNIT, row_w, lane, col_w, stage_ptr);
-                    else final_epilogue<float>(f, d, alpha / UNIT, row_w, lane, col_w, stage_ptr);
+                    if (c.x_bf16) final_epilogue<__nv_bfloat16, NC>(f, d, alpha / UNIT, row_w, lane, col_w, stage_ptr);
+                    else final_epilogue<float, NC>(f, d, alpha / UNIT, row_w, lane, col_w, stage_ptr);
                 }
             }
             release();
@@ -938,8 +998,9 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
                 // every lane's stores before the counts (which release them, by way of lane 0)
                 __syncwarp();
                 if (lane == 0) {
-                    const int place = u.op.out < 4 ? u.op.out * c.tiles_sq + u.ti * (u.ti + 1) / 2 + u.tj
-                                                   : 4 * c.tiles_sq + (u.op.out - 4) * c.tiles_x + u.ti * tiles_along(c.n) + u.tj;
+                    const int bj = u.tj / SH::Q;
+                    const int place = u.op.out < 4 ? u.op.out * c.blocks_sq + u.ti * (u.ti + 1) / 2 + bj
+                                                   : 4 * c.blocks_sq + (u.op.out - 4) * c.blocks_x + u.ti * SH::blocks(c.n) + bj;
                     asm volatile("fence.proxy.async;" ::: "memory");
                     asm volatile("fence.acq_rel.gpu;" ::: "memory");
                     asm volatile("red.relaxed.gpu.global.add.u32 [%0], 1;" ::"l"(c.tile_done + (int64_t)u.mat * c.counts + place) : "memory");
@@ -961,11 +1022,14 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
     }
     tc_fence_before();
     __syncthreads();
-    cluster_sync_all();
+    if (PAIR) cluster_sync_all();
     tc_fence_after();
     if (*abort_flag && threadIdx.x == 0)
         for (int i = 0; i < table.count; ++i) atomicOr(table.w[i].status, ST_WAIT);
-    if (warp == 1) tmem_dealloc_pair(tmem_base, 2 * TM);
+    if (warp == 1) {
+        if (PAIR) tmem_dealloc_pair(tmem_base, 2 * SH::COLS);
+        else tmem_dealloc(tmem_base, 2 * SH::COLS);
+    }
 }
 
 }  // namespace ns

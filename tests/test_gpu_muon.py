@@ -153,6 +153,24 @@ def test_grouped_call_gives_the_bits_of_single_calls():
         assert torch.equal(X, gx) and torch.equal(M, gm)
 
 
+@pytest.mark.parametrize("x", [BF16, F32])
+@pytest.mark.parametrize("m,n,count", [(257, 513, 9), (513, 257, 9), (700, 333, 5), (100, 37, 30), (520, 2056, 5), (1151, 1153, 2), (2049, 130, 26), (1800, 1800, 1)])
+def test_large_tiles(m, n, count, x):
+    """Calls with many tiles, which are larger then: against the definition, and the bits of calls with small ones (but where one matrix has
+    many tiles of its own)."""
+    hs = [plan(m, n, x=x)] * count
+    Gs = [gradient(("noise", "spikes", "decay")[i % 3], m, n, i, BF16) for i in range(count)]
+    Os = [torch.full((m, n), float("nan"), dtype=x, device="cuda") for _ in range(count)]
+    ws = workspace(hs)
+    od.orthdion_orthogonalize_grouped(od.MuonTable(hs, Os, None, Gs), ws)
+    assert od.orthdion_muon_last_status(count, ws) == [0] * count
+    for G, O in list(zip(Gs, Os))[:3]:
+        passes = 3 if x == F32 else 1
+        tol = min(STATED[passes], bound(G, [FAST] * 5, passes, x, exact_input=True))
+        assert rel(O, orthogonalise(G, [FAST] * 5)) <= tol
+        assert torch.equal(O, orth(G, x))
+
+
 def test_grouped_orthogonalise_and_in_place():
     shapes = [(64, 200), (200, 64), (64, 200)]
     hs = [plan(m, n) for m, n in shapes]
