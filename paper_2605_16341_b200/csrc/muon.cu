@@ -20,10 +20,7 @@ namespace {
 constexpr uint32_t kMuonMagic = 0x0D10B0E5u, kAdamWMagic = 0x0D10ADA3u;
 constexpr int32_t kMaxSteps = 32;
 constexpr size_t kScratchBudget = (size_t)4 << 30;     // per launch
-#ifndef OD_FEW
-#define OD_FEW 24
-#endif
-constexpr int kFewTiles = OD_FEW;
+constexpr double kFewProducts = 5e9;                    // see Launch::pair
 }  // namespace
 
 struct orthdion_muon_plan {
@@ -78,10 +75,12 @@ int terms_of(const orthdion_muon_plan* p) { return p->passes == 3 ? 2 : 1; }
 // while some directions have grown and others have not: not in the first two steps (all singular values are small after the division by
 // the norm) and not in the last two, but in between (noise and 32 strong directions, 129 x 1000, error of the result by grouping of five steps:
 // 2,2,1 8.1e-3; 1,2,2 2.8e-3; singles 2.5e-3; 2,1,2 2.3e-3; 2,1,1,1 2.2e-3).  A pair in front costs a square matrix nothing and saves
-// a rounding of X; one at the end pays where the matrix is longer than wide.
+// a rounding of X; one at the end pays where the matrix is longer than wide.  None with two terms, which need no care, where the number of products
+// counts, which is one less without a pair: up to 512 rows (256 x 512: 17 products 143 us, 15 126).
 struct Groups { int32_t pair_first, pair_last; };
 Groups group_steps(const orthdion_muon_plan* p) {
     const int64_t s = std::min(p->m, p->n), l = std::max(p->m, p->n);
+    if (p->passes == 3 && s <= 512) return Groups{0, 0};
     return Groups{p->steps >= 2, p->steps >= 5 && 4 * l >= 5 * s};
 }
 
@@ -101,7 +100,8 @@ Tiles tiles_of(const orthdion_muon_plan* p, bool pair) {
 
 // The scratch of `count` matrices of one plan: byte offsets, strides in elements.
 struct Scratch {
-    size_t slot, part, tile_done, x[2], sq[4], bytes;
+    size_t slot, tile_done, front;             // in the launch's front part, which is cleared: offsets and bytes
+    size_t part, x[2], sq[4], bytes;           // behind it
     int64_t x_pitch, x_term, x_mat, s_pitch, s_term, s_mat;
 };
 
@@ -112,10 +112,11 @@ Scratch scratch_layout(const orthdion_muon_plan* p, int count) {
     c.x_pitch = (int64_t)align_up(p->n, 64); c.x_term = p->m * c.x_pitch; c.x_mat = terms * c.x_term;
     c.s_pitch = (int64_t)align_up(s, 64); c.s_term = s * c.s_pitch; c.s_mat = terms * c.s_term;
     const Groups g = group_steps(p);
+    c.slot = 0;
+    c.tile_done = align_up(count * sizeof(ns::Slot), 256);
+    c.front = c.tile_done + align_up((size_t)count * std::max(tiles_of(p, true).counts(), tiles_of(p, false).counts()) * 4, 256);
     size_t off = 0;
-    c.slot = 0; off += align_up(count * sizeof(ns::Slot), 256);
-    c.part = off; off += align_up((size_t)count * ns::MAX_PARTS * 8, 1024);
-    c.tile_done = off; off += align_up((size_t)count * std::max(tiles_of(p, true).counts(), tiles_of(p, false).counts()) * 4, 1024);
+    c.part = off; off += align_up((size_t)count * 2 * ns::MAX_PARTS * 8, 1024);
     for (int i = 0; i < 2; ++i) {
         c.x[i] = off;
         if (i == 0 || p->steps > 1 + g.pair_first) off += align_up((size_t)count * c.x_mat * 2, 1024);
@@ -136,10 +137,13 @@ double cost(const orthdion_muon_plan* p) {
 // The launches of a call: matrices of up to MAX_CLASSES plans that are worked on together, as many as the scratch budget holds.
 struct Launch {
     std::vector<std::vector<int>> classes;     // matrices of one plan each
-    std::vector<size_t> off;                   // their scratch
-    size_t bytes = 0;
+    std::vector<size_t> front_off, off;        // their scratch: parts that are cleared, and the rest (behind all of those)
+    size_t front = 0, body = 0;
+    size_t bytes() const { return align_up(front, 1024) + body; }
     int matrices = 0;
-    bool pair = true;                          // tiles of CTA pairs, or of single CTAs
+    // Tiles of CTA pairs, or of single CTAs where s^2 l of all matrices comes to 5e9 at most: single and pair, us, 1024 x 1024 177, 225; 1536 x 1536
+    // 260, 265; 1280 x 4096 337, 337; two of 1024 x 4096 374, 339; four of 768 x 768 180, 208; with two terms 1536 x 1536 445, 550.
+    bool pair = true;
 };
 
 std::vector<Launch> make_launches(const orthdion_muon_t* hs, int32_t count, size_t* scratch) {
@@ -162,25 +166,31 @@ std::vector<Launch> make_launches(const orthdion_muon_t* hs, int32_t count, size
         const orthdion_muon_plan* p = hs[cls[0]];
         for (size_t at = 0; at < cls.size();) {
             if (out.empty() || terms != terms_of(p) || out.back().classes.size() == ns::MAX_CLASSES || out.back().matrices == ns::MAX_BATCH ||
-                out.back().bytes + scratch_layout(p, 1).bytes > kScratchBudget)
+                out.back().bytes() + scratch_layout(p, 1).bytes > kScratchBudget)
                 out.emplace_back();
             terms = terms_of(p);
             Launch& l = out.back();
             size_t n = std::min<size_t>(cls.size() - at, ns::MAX_BATCH - l.matrices);
-            while (n > 1 && l.bytes + scratch_layout(p, (int)n).bytes > kScratchBudget) --n;
+            while (n > 1 && l.bytes() + scratch_layout(p, (int)n).bytes > kScratchBudget) --n;
             l.classes.emplace_back(cls.begin() + at, cls.begin() + at + n);
-            l.off.push_back(l.bytes);
-            l.bytes += scratch_layout(p, (int)n).bytes;
+            const Scratch sc = scratch_layout(p, (int)n);
+            l.front_off.push_back(l.front);
+            l.off.push_back(l.body);
+            l.front += sc.front;
+            l.body += sc.bytes;
             l.matrices += (int)n;
             at += n;
         }
     }
     *scratch = 0;
     for (Launch& l : out) {
-        *scratch = std::max(*scratch, l.bytes);
-        int tiles = 0;             // of the symmetric products, 256 x 256
-        for (const auto& cls : l.classes) tiles += tiles_of(hs[cls[0]], true).sq * (int)cls.size();
-        l.pair = tiles > kFewTiles;
+        *scratch = std::max(*scratch, l.bytes());
+        double work = 0;
+        for (const auto& cls : l.classes) {
+            const orthdion_muon_plan* p = hs[cls[0]];
+            work += (double)cls.size() * std::min(p->m, p->n) * (double)(p->m * p->n);
+        }
+        l.pair = work > kFewProducts;
     }
     return out;
 }
@@ -213,6 +223,7 @@ void encode(ns::Class& c, int i, bool pair, const void* base, int64_t cols, int6
     }
 }
 
+int g_buffer_blocks[kMaxDevices] = {};    // blocks of the buffer kernel, likewise
 int g_at_once[kMaxDevices][2] = {};       // single CTAs and CTA pairs of the chain kernel that the device runs at once; written under ensure_attributes()'s lock
 
 int current_device() {
@@ -220,10 +231,39 @@ int current_device() {
     return cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < kMaxDevices ? dev : -1;
 }
 
+// by whether there is momentum, the gradient's type and whether there are whole vectors
+void (*const kBufferKernels[8])(ns::Table, ns::BufferArgs) = {
+    ns::buffer_kernel<ns::Form<false, false, false>>, ns::buffer_kernel<ns::Form<true, false, false>>, ns::buffer_kernel<ns::Form<false, true, false>>,
+    ns::buffer_kernel<ns::Form<true, true, false>>,   ns::buffer_kernel<ns::Form<false, false, true>>, ns::buffer_kernel<ns::Form<true, false, true>>,
+    ns::buffer_kernel<ns::Form<false, true, true>>,   ns::buffer_kernel<ns::Form<true, true, true>>};
+
+// A launch whose blocks wait for one another: all of them run at once, or none.
+template <class... KArgs, class... Args>
+void cooperative(void (*kernel)(KArgs...), int grid, int block, size_t smem, int cluster, int stage, cudaStream_t st, const Args&... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3((unsigned)block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeCooperative;
+    attr[0].val.cooperative = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = cluster > 1 ? 2 : 1;
+    prof::Scope scope(stage, st);
+    if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess && !engine_error()) engine_error() = LAUNCH_FAILED;
+}
+
 // One launch: the buffers' norms and images class by class, then all products.
 void run_launch(const orthdion_muon_t* hs, const Launch& l, void* const* X, float* const* M, const void* const* G, bool update, char* ws,
                 char* scratch, cudaStream_t st) {
     std::unique_ptr<ns::ChainArgs> args(new ns::ChainArgs());
+    struct Buffer {
+        ns::BufferArgs args{};
+        int32_t most_parts = 1, least_parts = ns::MAX_PARTS;
+    };
+    std::unique_ptr<Buffer[]> buffers(new Buffer[4]);
     ns::Table all{};
     const int terms = terms_of(hs[l.classes[0][0]]), at_once = g_at_once[current_device()][l.pair];
     args->classes = (int32_t)l.classes.size();
@@ -231,21 +271,20 @@ void run_launch(const orthdion_muon_t* hs, const Launch& l, void* const* X, floa
         const std::vector<int>& idx = l.classes[k];
         const orthdion_muon_plan* p = hs[idx[0]];
         const Scratch sc = scratch_layout(p, (int)idx.size());
-        char* base = scratch + l.off[k];
+        char *front = scratch + l.front_off[k], *base = scratch + align_up(l.front, 1024) + l.off[k];
         ns::Class& c = args->c[k];
-        ns::Table t{};
-        t.count = c.count = (int32_t)idx.size();
+        c.count = (int32_t)idx.size();
         c.first = all.count;
-        for (int i = 0; i < t.count; ++i) {
+        for (int i = 0; i < c.count; ++i) {
             const int j = idx[i];
-            t.w[i] = all.w[all.count++] = ns::Mat{G[j], update ? M[j] : nullptr, X[j], reinterpret_cast<int32_t*>(ws) + j};
+            all.w[all.count++] = ns::Mat{G[j], update ? M[j] : nullptr, X[j], reinterpret_cast<int32_t*>(ws) + j};
         }
         c.m = (int32_t)p->m; c.n = (int32_t)p->n;
         c.steps = p->steps;
         const Groups g = group_steps(p);
         c.pair_first = g.pair_first; c.pair_last = g.pair_last;
         std::memcpy(c.abc, p->abc, sizeof(c.abc));
-        c.slot = reinterpret_cast<ns::Slot*>(base + sc.slot);
+        c.slot = reinterpret_cast<ns::Slot*>(front + sc.slot);
         c.x_pitch = sc.x_pitch; c.x_term = sc.x_term; c.x_mat = sc.x_mat;
         c.s_pitch = sc.s_pitch; c.s_term = sc.s_term; c.s_mat = sc.s_mat;
         const int64_t s = std::min(p->m, p->n);
@@ -259,7 +298,7 @@ void run_launch(const orthdion_muon_t* hs, const Launch& l, void* const* X, floa
         }
         const Tiles tl = tiles_of(p, l.pair);
         c.tiles_sq = tl.sq; c.tiles_x = tl.x; c.blocks_sq = tl.blocks_sq; c.blocks_x = tl.blocks_x; c.counts = tl.counts();
-        c.tile_done = reinterpret_cast<uint32_t*>(base + sc.tile_done);
+        c.tile_done = reinterpret_cast<uint32_t*>(front + sc.tile_done);
         c.update = update;
         c.x_bf16 = p->x_dtype == ORTHDION_DTYPE_BF16;
         c.ld_x = p->ld_x;
@@ -268,46 +307,47 @@ void run_launch(const orthdion_muon_t* hs, const Launch& l, void* const* X, floa
         c.wc = 1.f - p->eta * p->wd; c.wd = p->eta * p->scale;
         args->stages = std::max(args->stages, ns::products(c.steps, c.pair_first, c.pair_last));
 
-        ns::PrepArgs a{};
+        // rows on 16-byte boundaries, and whole vectors
+        const bool vec = p->n % 8 == 0 && p->ld_g % 8 == 0 && (!update || p->ld_m % 4 == 0);
+        const int form = 2 * (p->g_dtype == ORTHDION_DTYPE_BF16) + vec;
+        Buffer& bu = buffers[form];
+        ns::PrepArgs& a = bu.args.c[bu.args.classes++];
+        bu.args.matrices += c.count;
         a.rows = p->m; a.cols = p->n; a.ld_g = p->ld_g; a.ld_m = p->ld_m;
-        a.g_bf16 = p->g_dtype == ORTHDION_DTYPE_BF16; a.nesterov = p->nesterov;
+        a.nesterov = p->nesterov;
         a.mu = (float)p->mu; a.rest = (float)(1.0 - p->mu);
         a.eps = p->eps;
         a.terms = terms;
-        a.vec = p->n % 8 == 0 && p->ld_g % 8 == 0 && (!update || p->ld_m % 4 == 0);
+        a.first = c.first; a.count = c.count;
         a.part = reinterpret_cast<double*>(base + sc.part);
         a.slot = c.slot;
-        a.counts = c.tile_done; a.counts_n = c.counts;
         a.img = c.x[0];
         a.pitch = sc.x_pitch; a.term_stride = sc.x_term; a.mat_stride = sc.x_mat;
-        // four chunks of 8 a thread, and no more blocks than eight per multiprocessor
-        const int64_t chunks = (p->n + 7) / 8 * p->m, most = std::max<int64_t>(1, 8 * sm_count() / t.count);
-        a.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({(chunks + 1023) / 1024, most, ns::MAX_PARTS}));
-        launch(ns::norm_kernel, dim3((unsigned)a.parts, (unsigned)t.count), 256, 0, 1, prof::S_NS_BUFFER, st, t, a);
-        const unsigned blocks = (unsigned)std::max<int64_t>(1, std::min<int64_t>((chunks + 1023) / 1024, most));
-        launch(ns::prep_kernel, dim3(blocks, (unsigned)t.count), 256, 0, 1, prof::S_NS_BUFFER, st, t, a);
+        // eight chunks of 8 columns a thread in a segment, more where there would be too many of them
+        const int64_t chunks = ns::chunks_per_row(p->n, vec) * p->m;
+        a.seg = std::max<int64_t>(8 * ns::BUFFER_THREADS, (int64_t)align_up((chunks + ns::MAX_PARTS - 1) / ns::MAX_PARTS, ns::BUFFER_THREADS));
+        a.parts = (int32_t)((chunks + a.seg - 1) / a.seg);
+        bu.most_parts = std::max(bu.most_parts, a.parts);
+        bu.least_parts = std::min(bu.least_parts, a.parts);
     }
     if (engine_error()) return;
+    if (cudaMemsetAsync(scratch, 0, l.front, st) != cudaSuccess) { engine_error() = LAUNCH_FAILED; return; }
+    for (int form = 0; form < 4; ++form) {
+        Buffer& bu = buffers[form];
+        if (!bu.args.classes) continue;
+        // A team has as many blocks as the smallest matrix has segments, or its share of the blocks where there are few matrices.
+        const int blocks = g_buffer_blocks[current_device()], matrices = bu.args.matrices;
+        bu.args.team = std::min({blocks, bu.most_parts, std::max(bu.least_parts, blocks / matrices)});
+        cooperative(kBufferKernels[4 * update + form], std::min(matrices, blocks / bu.args.team) * bu.args.team, ns::BUFFER_THREADS, 0, 1,
+                    prof::S_NS_BUFFER, st, all, bu.args);
+    }
 
     int units = 0;                 // of the products with the most tiles
     for (int k = 0; k < args->classes; ++k) units += std::max(args->c[k].tiles_sq, args->c[k].tiles_x) * args->c[k].count;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)((l.pair ? 2 : 1) * std::min(at_once, units)));
-    cfg.blockDim = dim3(ns::THREADS);
-    cfg.dynamicSmemBytes = ns::SMEM_BYTES;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = l.pair ? 2 : 1; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    // (pairs wait for one another's tiles: all of them run at once, or none)
-    attr[1].id = cudaLaunchAttributeCooperative;
-    attr[1].val.cooperative = 1;
-    cfg.attrs = attr; cfg.numAttrs = 2;
-    prof::Scope scope(prof::S_NS_PRODUCT, st);
     const auto kernel = l.pair ? (terms == 2 ? ns::chain_kernel<true, 2> : ns::chain_kernel<true, 1>)
                                : (terms == 2 ? ns::chain_kernel<false, 2> : ns::chain_kernel<false, 1>);
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, all, *args);
-    if (e != cudaSuccess) engine_error() = LAUNCH_FAILED;
+    const int ctas = l.pair ? 2 : 1;
+    cooperative(kernel, ctas * std::min(at_once, units), ns::THREADS, ns::SMEM_BYTES, ctas, prof::S_NS_PRODUCT, st, all, *args);
 }
 
 int ensure_attributes() {
@@ -332,6 +372,12 @@ int ensure_attributes() {
         if (e == cudaSuccess && n < 1) e = cudaErrorInvalidConfiguration;
         g_at_once[dev][pair] = g_at_once[dev][pair] ? std::min(g_at_once[dev][pair], n) : n;
     };
+    int per_sm = 0;
+    for (auto* kernel : kBufferKernels) {
+        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, ns::BUFFER_THREADS, 0);
+        const int n = std::max(1, std::min(per_sm, ns::BUFFER_BLOCKS)) * sm_count();
+        g_buffer_blocks[dev] = g_buffer_blocks[dev] ? std::min(g_buffer_blocks[dev], n) : n;
+    }
     set(ns::chain_kernel<true, 1>, true);
     set(ns::chain_kernel<true, 2>, true);
     set(ns::chain_kernel<false, 1>, false);
@@ -379,7 +425,6 @@ int run_call(const orthdion_muon_t* hs, int32_t count, void* const* X, float* co
     if (e) return e;
     char* ws = reinterpret_cast<char*>(workspace);
     engine_error() = 0;
-    overlap_launches() = true;
     for (const Launch& l : launches) {
         run_launch(hs, l, X, M, G, update, ws, ws + status_bytes(count), reinterpret_cast<cudaStream_t>(stream));
         if (engine_error()) break;

@@ -26,7 +26,8 @@ using namespace od::tc;
 
 constexpr float UNIT = 256.f;            // images hold UNIT times the value
 constexpr int MAX_BATCH = 64;            // matrices of one launch (its table: 2 KB of kernel parameters)
-constexpr int MAX_PARTS = 512;           // partial sums of squares of one matrix
+constexpr int MAX_PARTS = 2048;          // partial sums of squares of one matrix
+constexpr int MAX_CLASSES = 6;           // plans of one launch (their maps and the rest come to 24 KB of kernel parameters)
 
 // The caller's buffers of one matrix.
 struct Mat {
@@ -44,181 +45,182 @@ struct Slot {
     float sigma;       // UNIT / (stored |X0| + stored eps): how much larger the normalised matrix is than the stored one
     int32_t status;
     uint32_t done;     // epilogue warps that have finished a tile of one of its products
-    int32_t pad;
+    uint32_t summed;   // blocks that have finished their share of the norm
 };
 
 // ---- the buffer B, its norm, its image ---------------------------------------------------------
 struct PrepArgs {
     int64_t rows, cols, ld_g, ld_m;
-    int32_t g_bf16, nesterov;
+    int32_t nesterov;
     float mu, rest;              // momentum, 1 - momentum
     double eps;
-    int32_t parts, terms;
-    int32_t vec;                 // rows start on 16-byte boundaries
-    double* part;                // [matrix][MAX_PARTS]
-    Slot* slot;
-    uint32_t* counts;            // [matrix][counts_n], cleared
-    int32_t counts_n;
+    int32_t first, count;        // matrices of the table
+    int32_t terms, parts;
+    int64_t seg;                 // chunks of one partial sum (by the matrix's size alone: the same sums in whatever call it stands)
+    double* part;                // [matrix][2][MAX_PARTS]
+    Slot* slot;                  // cleared
     __half* img;
     int64_t pitch, term_stride, mat_stride;      // of the image, in elements
 };
+// Chunks of 8 entries in a row (the last ones may lie beyond its end).
+__host__ __device__ inline int64_t chunks_per_row(int64_t cols, bool vec) { return vec ? (cols + 7) / 8 : (cols + 255) / 256 * 32; }
+struct BufferArgs {
+    int32_t classes, matrices, team;       // team: blocks that work on one matrix together
+    PrepArgs c[MAX_CLASSES];
+};
 
-// 8 entries of G and M at (row, col) as they lie in memory; zeros beyond the last column.
-struct Raw { uint4 g[2], m[2]; };
-template <bool VEC>
-__device__ __forceinline__ void load_raw(const Mat& w, const PrepArgs& a, int64_t row, int64_t col, Raw& r) {
+// 8 entries of G and M from (row, col) as they lie in memory: one after the other, or 32 columns apart where rows start on no 16-byte boundary (the
+// lanes of a warp then take neighbouring ones); zeros beyond the last column.
+// What a buffer kernel is made for.  VEC: rows start on 16-byte boundaries, and have whole vectors.  MOMENTUM: B comes from G and M, else from G alone.
+template <bool VEC_, bool G_BF16_, bool MOMENTUM_>
+struct Form { static constexpr bool VEC = VEC_, G_BF16 = G_BF16_, MOMENTUM = MOMENTUM_; };
+template <class F>
+struct Raw {
+    uint4 g[F::G_BF16 ? 1 : 2], m[F::MOMENTUM ? 2 : 1];
+};
+template <class F>
+__device__ __forceinline__ void load_raw(const Mat& w, const PrepArgs& a, int64_t row, int64_t col, Raw<F>& r) {
     const int64_t gi = row * a.ld_g + col, mi = row * a.ld_m + col;
-    if (VEC) {
-        if (a.g_bf16) {
-            r.g[0] = *reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(w.G) + gi);
-        } else {
-            const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const float*>(w.G) + gi);
-            r.g[0] = p[0]; r.g[1] = p[1];
-        }
-        if (w.M) {
-            const uint4* p = reinterpret_cast<const uint4*>(w.M + mi);
-            r.m[0] = p[0]; r.m[1] = p[1];
+    if (F::VEC) {
+        const uint4* p = F::G_BF16 ? reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(w.G) + gi)
+                                   : reinterpret_cast<const uint4*>(reinterpret_cast<const float*>(w.G) + gi);
+        r.g[0] = p[0];
+        if (!F::G_BF16) r.g[F::G_BF16 ? 0 : 1] = p[1];
+        if (F::MOMENTUM) {
+            const uint4* q = reinterpret_cast<const uint4*>(w.M + mi);
+            r.m[0] = q[0]; r.m[F::MOMENTUM ? 1 : 0] = q[1];
         }
     } else {
         uint32_t* gw = reinterpret_cast<uint32_t*>(r.g);
         uint32_t* mw = reinterpret_cast<uint32_t*>(r.m);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const bool in = col + e < a.cols;
-            if (a.g_bf16) {
-                const uint32_t v = in ? reinterpret_cast<const uint16_t*>(w.G)[gi + e] : 0u;
+            const bool in = col + 32 * e < a.cols;
+            if (F::G_BF16) {
+                const uint32_t v = in ? reinterpret_cast<const uint16_t*>(w.G)[gi + 32 * e] : 0u;
                 if (e % 2) gw[e / 2] |= v << 16;
                 else gw[e / 2] = v;
             } else {
-                gw[e] = in ? reinterpret_cast<const uint32_t*>(w.G)[gi + e] : 0u;
+                gw[e] = in ? reinterpret_cast<const uint32_t*>(w.G)[gi + 32 * e] : 0u;
             }
-            if (w.M) mw[e] = in ? reinterpret_cast<const uint32_t*>(w.M)[mi + e] : 0u;
+            if (F::MOMENTUM) mw[e] = in ? reinterpret_cast<const uint32_t*>(w.M)[mi + 32 * e] : 0u;
         }
     }
 }
 // Those 8 entries of B, and of the updated momentum.
-__device__ __forceinline__ void buffer_of(const Raw& r, const PrepArgs& a, bool momentum, float (&b)[8], float (&m)[8]) {
-    const uint32_t gw[8] = {r.g[0].x, r.g[0].y, r.g[0].z, r.g[0].w, r.g[1].x, r.g[1].y, r.g[1].z, r.g[1].w};
-    const uint32_t mw[8] = {r.m[0].x, r.m[0].y, r.m[0].z, r.m[0].w, r.m[1].x, r.m[1].y, r.m[1].z, r.m[1].w};
+template <class F>
+__device__ __forceinline__ void buffer_of(const Raw<F>& r, const PrepArgs& a, float (&b)[8], float (&m)[8]) {
+    const uint32_t* gw = reinterpret_cast<const uint32_t*>(r.g);
+    const uint32_t* mw = reinterpret_cast<const uint32_t*>(r.m);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const float g = a.g_bf16 ? (e % 2 ? bf16hi_to_f32(gw[e / 2]) : bf16lo_to_f32(gw[e / 2])) : __uint_as_float(gw[e]);
-        if (!momentum) { b[e] = g; continue; }
+        const float g = F::G_BF16 ? (e % 2 ? bf16hi_to_f32(gw[e / 2]) : bf16lo_to_f32(gw[e / 2])) : __uint_as_float(gw[e]);
+        if (!F::MOMENTUM) { b[e] = g; continue; }
         // (the same instructions wherever B is formed: the same bits)
         m[e] = __fmaf_rn(a.mu, __uint_as_float(mw[e]), __fmul_rn(a.rest, g));
         b[e] = a.nesterov ? __fmaf_rn(a.mu, m[e], __fmul_rn(a.rest, g)) : m[e];
     }
 }
 
-// Walks the 8-column chunks of the matrix that this block takes of `blocks`, U of them loaded before the first is used (one at a time:
-// 16 us for a sweep over a 4096 x 4096 bf16 matrix).
-template <int U, bool VEC, class F>
-__device__ __forceinline__ void for_chunks(const Mat& w, const PrepArgs& a, int block, int blocks, F f) {
-    const int64_t cpr = (a.cols + 7) / 8, total = cpr * a.rows, step = (int64_t)blocks * blockDim.x;
-    int64_t i = (int64_t)block * blockDim.x + threadIdx.x;
-    int64_t row = i / cpr, c = i - row * cpr;
-    const int64_t drow = step / cpr, dc = step - drow * cpr;
-    while (i < total) {
-        Raw r[U];
-        int64_t rows[U], cols[U];
-        int n = 0;
+#ifndef OD_WU
+#define OD_WU 4
+#endif
+constexpr int WRITE_U = OD_WU;
+constexpr int BUFFER_THREADS = 256, BUFFER_BLOCKS = 2;       // of a multiprocessor
+
+// f(entries, row, column) for the chunks of segment `seg` that this thread takes, U of them loaded before the first is used.
+template <int U, class FORM, class F>
+__device__ __forceinline__ void for_chunks(const Mat& w, const PrepArgs& a, int seg, F f) {
+    const int64_t cpr = chunks_per_row(a.cols, FORM::VEC), begin = seg * a.seg, first = begin + threadIdx.x;
+    auto column = [](int c) { return FORM::VEC ? c * 8 : c / 32 * 256 + c % 32; };
+    int left = (int)min(a.seg, cpr * a.rows - begin) - (int)threadIdx.x;       // chunks from this thread's next one to the end
+    const int width = (int)cpr, drow = BUFFER_THREADS / width, dc = BUFFER_THREADS - drow * width;
+    int row = (int)(first / cpr), c = (int)(first - row * cpr);
+    auto next = [&] {
+        left -= BUFFER_THREADS; row += drow; c += dc;
+        if (c >= width) { c -= width; ++row; }
+    };
+    while (left > (U - 1) * BUFFER_THREADS) {
+        Raw<FORM> r[U];
+        int rows[U], cols[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (i < total) {
-                rows[u] = row; cols[u] = c * 8;
-                load_raw<VEC>(w, a, row, c * 8, r[u]);
-                n = u + 1;
-            }
-            i += step; row += drow; c += dc;
-            if (c >= cpr) { c -= cpr; ++row; }
+            rows[u] = row; cols[u] = column(c);
+            load_raw<FORM>(w, a, row, cols[u], r[u]);
+            next();
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (u < n) f(r[u], rows[u], cols[u]);
+        for (int u = 0; u < U; ++u) f(r[u], rows[u], cols[u]);
+    }
+#pragma unroll 1
+    while (left > 0) {
+        Raw<FORM> r;
+        load_raw<FORM>(w, a, row, column(c), r);
+        f(r, row, column(c));
+        next();
     }
 }
 
 __device__ __forceinline__ double block_sum(double v, double* red) {
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    __syncthreads();
     if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = v;
     __syncthreads();
     v = 0.0;
-    for (int i = 0; i < (int)blockDim.x / 32; ++i) v += red[i];
+#pragma unroll
+    for (int i = 0; i < BUFFER_THREADS / 32; ++i) v += red[i];
     return v;
 }
 
-// Sums of squares of B, one per block, in 64 bits (a sum over up to 10^8 entries, and squares of any finite entry).
-__global__ void __launch_bounds__(256) norm_kernel(const __grid_constant__ Table t, const __grid_constant__ PrepArgs a) {
-    __shared__ double red[8];
-    grid_dependency();
-    const Mat& w = t.w[blockIdx.y];
+template <class FORM, bool WIDE>
+__device__ __forceinline__ double sum_segment(const Mat& w, const PrepArgs& a, int seg) {
     double sum = 0.0;
-    auto add = [&](const Raw& r, int64_t, int64_t) {
+    for_chunks<FORM::VEC && !WIDE ? 4 : 1, FORM>(w, a, seg, [&](const Raw<FORM>& r, int, int) {
         float b[8], m[8];
-        buffer_of(r, a, w.M != nullptr, b, m);
-        // eight squares in 32 bits (2^-22 of them at most), unless they overflow or come near what vanishes
-        float q = b[0] * b[0];
+        buffer_of<FORM>(r, a, b, m);
+        if (WIDE) {
 #pragma unroll
-        for (int e = 1; e < 8; ++e) q = fmaf(b[e], b[e], q);
-        if (q >= 1e-28f && q <= 1e38f) {
-            sum += (double)q;
-        } else {
-#pragma unroll 1
             for (int e = 0; e < 8; ++e) sum = fma((double)b[e], (double)b[e], sum);
+        } else {
+            float q = b[0] * b[0];                   // eight squares in 32 bits
+#pragma unroll
+            for (int e = 1; e < 8; ++e) q = fmaf(b[e], b[e], q);
+            sum += (double)q;
         }
-    };
-    if (a.vec) for_chunks<4, true>(w, a, blockIdx.x, a.parts, add);
-    else for_chunks<2, false>(w, a, blockIdx.x, a.parts, add);
-    sum = block_sum(sum, red);
-    if (threadIdx.x == 0) a.part[(int64_t)blockIdx.y * MAX_PARTS + blockIdx.x] = sum;
+    });
+    return sum;
 }
-
-// The image of B, scaled by the power of two that brings its norm to [128, 256) (a gradient in bf16 is then held exactly; what is left
-// of the normalisation, sigma, goes into the factors of the first products), and the updated momentum.  A matrix whose norm is
-// not finite keeps its momentum.
-__global__ void __launch_bounds__(256) prep_kernel(const __grid_constant__ Table t, const __grid_constant__ PrepArgs a) {
-    __shared__ double red[8];
-    grid_dependency();
-    const Mat& w = t.w[blockIdx.y];
-    double sum = 0.0;
-    for (int i = threadIdx.x; i < a.parts; i += blockDim.x) sum += a.part[(int64_t)blockIdx.y * MAX_PARTS + i];
-    sum = block_sum(sum, red);
-    const double norm = sqrt(sum);
-    const bool finite = norm <= 1.7e308;
-    int e = 0;
-    if (finite && norm > 0.0) frexp(norm, &e);
-    const int k = finite && norm > 0.0 ? 8 - e : 0;
-    // (the power itself may be beyond fp32, so two factors)
-    const float f1 = ldexpf(1.f, k / 2), f2 = ldexpf(1.f, k - k / 2);
-    if (blockIdx.x == 0 && threadIdx.x == 0) {
-        Slot s{};
-        s.sigma = finite && norm > 0.0 ? (float)((double)UNIT / ldexp(norm + a.eps, k)) : 0.f;
-        s.status = finite ? 0 : ST_NONFINITE;
-        a.slot[blockIdx.y] = s;
-        *w.status = s.status;
-    }
-    for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < a.counts_n; i += gridDim.x * blockDim.x) a.counts[(int64_t)blockIdx.y * a.counts_n + i] = 0;
-    if (!finite) return;
-    __half* img = a.img + (int64_t)blockIdx.y * a.mat_stride;
-    auto write = [&](const Raw& r, int64_t row, int64_t col) {
+template <class FORM>
+__device__ __forceinline__ void write_segment(const Mat& w, const PrepArgs& a, int seg, __half* img, float f1, float f2) {
+    for_chunks<FORM::VEC ? WRITE_U : 1, FORM>(w, a, seg, [&](const Raw<FORM>& r, int row, int col) {
         float b[8], m[8];
-        buffer_of(r, a, w.M != nullptr, b, m);
-        if (w.M) {
+        buffer_of<FORM>(r, a, b, m);
+        if (FORM::MOMENTUM) {
             float* dst = w.M + row * a.ld_m + col;
-            if (a.vec) {
+            if (FORM::VEC) {
                 reinterpret_cast<float4*>(dst)[0] = make_float4(m[0], m[1], m[2], m[3]);
                 reinterpret_cast<float4*>(dst)[1] = make_float4(m[4], m[5], m[6], m[7]);
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (col + i < a.cols) dst[i] = m[i];
+                    if (col + 32 * i < a.cols) dst[32 * i] = m[i];
             }
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) b[i] = b[i] * f1 * f2;
         __half* dst = img + row * a.pitch + col;
         const uint4 hi = half8(b, 1.f);
-        *reinterpret_cast<uint4*>(dst) = hi;
+        auto store = [&](__half* to, const uint4& v) {
+            if (FORM::VEC) {
+                *reinterpret_cast<uint4*>(to) = v;
+            } else {
+                const uint32_t h[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (col + 32 * i < a.cols) reinterpret_cast<uint16_t*>(to)[32 * i] = (uint16_t)(h[i / 2] >> (i % 2 * 16));
+            }
+        };
+        store(dst, hi);
         if (a.terms == 2) {
             const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
@@ -226,11 +228,73 @@ __global__ void __launch_bounds__(256) prep_kernel(const __grid_constant__ Table
                 const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
                 b[2 * i] -= v.x; b[2 * i + 1] -= v.y;
             }
-            *reinterpret_cast<uint4*>(dst + a.term_stride) = half8(b, 1.f);
+            store(dst + a.term_stride, half8(b, 1.f));
         }
-    };
-    if (a.vec) for_chunks<4, true>(w, a, blockIdx.x, gridDim.x, write);
-    else for_chunks<2, false>(w, a, blockIdx.x, gridDim.x, write);
+    });
+}
+
+// What is left of one matrix when the last block of its team has summed: the image of B, scaled by the power of two that brings its norm to
+// [128, 256) (a gradient in bf16 is then held exactly; what is left of the normalisation, sigma, goes into the factors of the first products), and
+// the updated momentum.  A matrix whose norm is not finite keeps its momentum.  The second look at B finds most of it in L2: a team
+// works on one matrix at a time and goes back over it the way it came.  (As two launches, norms of all matrices and then images, the seven
+// matrices of a layer of a 1.1B model took 225 us, 18 bytes an entry at 4.1 TB/s.)  The squares are summed in 64 bits.
+template <class FORM>
+__global__ void __launch_bounds__(BUFFER_THREADS, BUFFER_BLOCKS) buffer_kernel(const __grid_constant__ Table t, const __grid_constant__ BufferArgs g) {
+    __shared__ double red[BUFFER_THREADS / 32];
+    __shared__ int failed;
+    grid_dependency();
+    const int rank = (int)blockIdx.x % g.team, teams = (int)gridDim.x / g.team;
+    int cls = 0, before = 0;
+    for (int k = (int)blockIdx.x / g.team; k < g.matrices; k += teams) {
+        while (k >= before + g.c[cls].count) before += g.c[cls++].count;
+        const PrepArgs& a = g.c[cls];
+        const int mat = k - before;
+        const Mat& w = t.w[a.first + mat];
+        Slot* slot = a.slot + mat;
+        double* part = a.part + (int64_t)mat * (2 * MAX_PARTS);
+        double sum = 0.0;
+        // Once with squares in 32 bits, eight at a time; where the sum says that some overflowed or most of it vanished, all in 64.
+        for (int wide = 0; wide < 2; ++wide) {
+            for (int seg = rank; seg < a.parts; seg += g.team) {
+                const double mine = wide ? sum_segment<FORM, true>(w, a, seg) : sum_segment<FORM, false>(w, a, seg);
+                const double all = block_sum(mine, red);
+                if (threadIdx.x == 0) __stcg(part + wide * MAX_PARTS + seg, all);
+            }
+            if (threadIdx.x == 0) {
+                const uint32_t want = (uint32_t)(g.team * (wide + 1));
+                uint32_t v = 0;
+                asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(&slot->summed) : "memory");
+                const long long t0 = clock64();
+                do {
+                    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(&slot->summed) : "memory");
+                } while ((int32_t)(v - want) < 0 && clock64() - t0 < WAIT_LIMIT_CYCLES);
+                failed = (int32_t)(v - want) < 0;
+            }
+            __syncthreads();
+            sum = 0.0;
+            for (int i = threadIdx.x; i < a.parts; i += BUFFER_THREADS) sum += __ldcg(part + wide * MAX_PARTS + i);
+            sum = block_sum(sum, red);
+            if (failed || (sum >= 1e-20 && sum <= 1.7e308)) break;
+        }
+        const double norm = sqrt(sum);
+        const bool finite = norm <= 1.7e308;
+        int e = 0;
+        if (finite && norm > 0.0) frexp(norm, &e);
+        const int p2 = finite && norm > 0.0 ? 8 - e : 0;
+        // (the power itself may be beyond fp32, so two factors)
+        const float f1 = ldexpf(1.f, p2 / 2), f2 = ldexpf(1.f, p2 - p2 / 2);
+        if (threadIdx.x == 0 && (rank == 0 || failed)) {
+            slot->sigma = finite && norm > 0.0 ? (float)((double)UNIT / ldexp(norm + a.eps, p2)) : 0.f;
+            slot->status = failed ? ST_WAIT : finite ? 0 : ST_NONFINITE;
+            *w.status = slot->status;
+        }
+        if (failed) return;
+        if (!finite) continue;
+        __half* img = a.img + (int64_t)mat * a.mat_stride;
+        for (int seg = a.parts - 1 - (a.parts - 1 - rank + g.team) % g.team; seg >= 0; seg -= g.team) {
+            write_segment<FORM>(w, a, seg, img, f1, f2);
+        }
+    }
 }
 
 // ---- the products: one persistent kernel for all steps of a batch ------------------------------------
@@ -276,7 +340,6 @@ struct Shape {
     __host__ __device__ static constexpr int width(int block, int n) { return tiles(n) - Q * block < Q ? tiles(n) - Q * block : Q; }
 };
 constexpr int GROUP_ROWS = 8;                 // tile rows that are walked together, column by column
-constexpr int MAX_CLASSES = 6;                // (their maps and the rest come to 24 KB of kernel parameters)
 constexpr int MAX_ITER = 32;                  // steps of a schedule
 
 // Matrices of one plan.

@@ -52,10 +52,12 @@ def bound(B, schedule, passes, x_dtype, eps=1e-7, exact_input=False):
 
     eye = torch.eye(s, dtype=torch.float64, device=X.device)
     err = (0.0 if exact_input and passes == 1 else u * fro(X)) + 2.0 ** -23 * fro(X)      # the scale that is left is rounded too
-    # steps between two roundings of X: two in front, and two at the end of five or more where the matrix is longer than wide
-    k, pair_last = 0, len(schedule) >= 5 and 4 * l >= 5 * s
+    # steps between two roundings of X: two in front, and two at the end of five or more where the matrix is longer than wide;
+    # one by one where a small matrix has two-term operands
+    singles = passes == 3 and s <= 512
+    k, pair_last = 0, len(schedule) >= 5 and 4 * l >= 5 * s and not singles
     while k < len(schedule):
-        steps = schedule[k:k + (2 if k == 0 or (pair_last and len(schedule) - k == 2) else 1)]
+        steps = schedule[k:k + (2 if (k == 0 and not singles) or (pair_last and len(schedule) - k == 2) else 1)]
         A = X @ X.T
         dA = u * fro(A) + gamma(l) * fro(X) ** 2 + 2.0 ** -22 * fro(A)
         P = dP = None
