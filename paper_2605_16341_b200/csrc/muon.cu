@@ -323,9 +323,9 @@ void run_launch(const orthdion_muon_t* hs, const Launch& l, void* const* X, floa
         a.slot = c.slot;
         a.img = c.x[0];
         a.pitch = sc.x_pitch; a.term_stride = sc.x_term; a.mat_stride = sc.x_mat;
-        // eight chunks of 8 columns a thread in a segment, more where there would be too many of them
+        // four chunks a thread in a segment, more where there would be too many of them
         const int64_t chunks = ns::chunks_per_row(p->n, vec) * p->m;
-        a.seg = std::max<int64_t>(8 * ns::BUFFER_THREADS, (int64_t)align_up((chunks + ns::MAX_PARTS - 1) / ns::MAX_PARTS, ns::BUFFER_THREADS));
+        a.seg = std::max<int64_t>(4 * ns::BUFFER_THREADS, (int64_t)align_up((chunks + ns::MAX_PARTS - 1) / ns::MAX_PARTS, ns::BUFFER_THREADS));
         a.parts = (int32_t)((chunks + a.seg - 1) / a.seg);
         bu.most_parts = std::max(bu.most_parts, a.parts);
         bu.least_parts = std::min(bu.least_parts, a.parts);
@@ -335,10 +335,11 @@ void run_launch(const orthdion_muon_t* hs, const Launch& l, void* const* X, floa
     for (int form = 0; form < 4; ++form) {
         Buffer& bu = buffers[form];
         if (!bu.args.classes) continue;
-        // A team has as many blocks as the smallest matrix has segments, or its share of the blocks where there are few matrices.
+        // As many teams as there are matrices, but of blocks enough that each has a segment of the smallest one.
         const int blocks = g_buffer_blocks[current_device()], matrices = bu.args.matrices;
-        bu.args.team = std::min({blocks, bu.most_parts, std::max(bu.least_parts, blocks / matrices)});
-        cooperative(kBufferKernels[4 * update + form], std::min(matrices, blocks / bu.args.team) * bu.args.team, ns::BUFFER_THREADS, 0, 1,
+        const int teams = std::max(1, std::min(matrices, blocks / bu.least_parts));
+        bu.args.team = std::min(bu.most_parts, blocks / teams);
+        cooperative(kBufferKernels[4 * update + form], teams * bu.args.team, ns::BUFFER_THREADS, 0, 1,
                     prof::S_NS_BUFFER, st, all, bu.args);
     }
 

@@ -122,11 +122,8 @@ __device__ __forceinline__ void buffer_of(const Raw<F>& r, const PrepArgs& a, fl
     }
 }
 
-#ifndef OD_WU
-#define OD_WU 4
-#endif
-constexpr int WRITE_U = OD_WU;
-constexpr int BUFFER_THREADS = 256, BUFFER_BLOCKS = 2;       // of a multiprocessor
+constexpr int BUFFER_THREADS = 256, BUFFER_BLOCKS = 4;       // of a multiprocessor
+constexpr int BUFFER_U = 2;                                  // chunks under way in a thread
 
 // f(entries, row, column) for the chunks of segment `seg` that this thread takes, U of them loaded before the first is used.
 template <int U, class FORM, class F>
@@ -175,7 +172,7 @@ __device__ __forceinline__ double block_sum(double v, double* red) {
 template <class FORM, bool WIDE>
 __device__ __forceinline__ double sum_segment(const Mat& w, const PrepArgs& a, int seg) {
     double sum = 0.0;
-    for_chunks<FORM::VEC && !WIDE ? 4 : 1, FORM>(w, a, seg, [&](const Raw<FORM>& r, int, int) {
+    for_chunks<FORM::VEC && !WIDE ? BUFFER_U : 1, FORM>(w, a, seg, [&](const Raw<FORM>& r, int, int) {
         float b[8], m[8];
         buffer_of<FORM>(r, a, b, m);
         if (WIDE) {
@@ -192,7 +189,7 @@ __device__ __forceinline__ double sum_segment(const Mat& w, const PrepArgs& a, i
 }
 template <class FORM>
 __device__ __forceinline__ void write_segment(const Mat& w, const PrepArgs& a, int seg, __half* img, float f1, float f2) {
-    for_chunks<FORM::VEC ? WRITE_U : 1, FORM>(w, a, seg, [&](const Raw<FORM>& r, int row, int col) {
+    for_chunks<FORM::VEC ? BUFFER_U : 1, FORM>(w, a, seg, [&](const Raw<FORM>& r, int row, int col) {
         float b[8], m[8];
         buffer_of<FORM>(r, a, b, m);
         if (FORM::MOMENTUM) {
