@@ -860,6 +860,7 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
                 const uint32_t missing = __ballot_sync(0xffffffffu, !there);
                 const int tiles = missing ? __ffs(missing) - 1 : 32;
                 if (tiles) {
+                    // (here and not in the producer, which it holds up for half a microsecond a unit)
                     asm volatile("fence.acq_rel.gpu;" ::: "memory");
                     asm volatile("fence.proxy.async;" ::: "memory");
                     __syncwarp();
@@ -894,7 +895,6 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
                         if ((spins & 63) == 63 && (*abort_flag || clock64() - t0 > WAIT_LIMIT_CYCLES)) { *abort_flag = 1; ok = false; break; }
                     }
                     if (!ok) break;
-                    asm volatile("fence.proxy.async;" ::: "memory");
                     int end = min(ready - total, kblocks);
                     if (kb < a_turn) end = min(end, a_turn);
                     if (kb < b_turn) end = min(end, b_turn);
