@@ -26,7 +26,7 @@ using namespace od::tc;
 
 constexpr float UNIT = 256.f;            // images hold UNIT times the value
 constexpr int MAX_BATCH = 64;            // matrices of one launch (its table: 2 KB of kernel parameters)
-constexpr int MAX_PARTS = 2048;          // partial sums of squares of one matrix
+constexpr int MAX_PARTS = 1024;          // partial sums of squares of one matrix
 constexpr int MAX_CLASSES = 6;           // plans of one launch (their maps and the rest come to 24 KB of kernel parameters)
 
 // The caller's buffers of one matrix.
@@ -269,7 +269,9 @@ __global__ void __launch_bounds__(BUFFER_THREADS, BUFFER_BLOCKS) buffer_kernel(c
             }
             __syncthreads();
             sum = 0.0;
-            for (int i = threadIdx.x; i < a.parts; i += BUFFER_THREADS) sum += __ldcg(part + wide * MAX_PARTS + i);
+#pragma unroll
+            for (int i = 0; i < MAX_PARTS; i += BUFFER_THREADS)
+                if (i + (int)threadIdx.x < a.parts) sum += __ldcg(part + wide * MAX_PARTS + i + threadIdx.x);
             sum = block_sum(sum, red);
             if (failed || (sum >= 1e-20 && sum <= 1.7e308)) break;
         }
