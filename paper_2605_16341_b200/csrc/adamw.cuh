@@ -1,4 +1,6 @@
-// The AdamW step of tensors of any length: one pass over X, G and both moments.
+// The AdamW step of tensors of any length: one pass over X, G and both moments, bound by HBM.  A block takes one piece of one tensor, two groups of
+// eight entries a thread: 65.5 M bf16 entries (1.44 GB) in 216 us, 6.65 TB/s; with 1184 blocks that walk over the pieces 255 us (they all
+// wait for their loads at once), with one group a thread 237, with streaming hints on loads and stores 242 to 265.
 #pragma once
 #include "common.cuh"
 #include "launch.cuh"
@@ -6,10 +8,10 @@
 namespace od {
 namespace adamw {
 
-constexpr int MAX_TENSORS = 64;          // of one launch (its table: 3.5 KB of kernel parameters)
+constexpr int MAX_TENSORS = 96;          // of one launch (its table: 5.5 KB of kernel parameters)
 constexpr int MAX_KINDS = 8;             // different constants among them
-constexpr int THREADS = 256;
-constexpr int CHUNK = 8 * THREADS * 2;   // entries that one block takes at a time
+constexpr int THREADS = 256, GROUPS = 2;
+constexpr int CHUNK = 8 * THREADS * GROUPS;   // entries of one block
 
 struct Tensor {
     void* X;
@@ -26,7 +28,7 @@ struct Kind {
 struct Table {
     int32_t count, chunks;
     int64_t* step;                       // [0]: steps taken, [1]: blocks of this step that are done
-    int32_t last, blocks;                // last: this launch ends the step
+    int32_t last, pad;                   // last: this launch ends the step
     Kind kind[MAX_KINDS];
     Tensor t[MAX_TENSORS];
 };
@@ -58,50 +60,53 @@ __device__ __forceinline__ void update(const Consts& k, float& x, float& m, floa
 
 template <bool X_BF16, bool G_BF16>
 __global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ Table a) {
-    __shared__ Consts consts[MAX_KINDS];
+    __shared__ float correction[2];
     grid_dependency();
-    // the bias corrections in 64 bits: 1 - beta^t of a beta near 1 loses most of 24
-    if (threadIdx.x < MAX_KINDS) {
-        const Kind& k = a.kind[threadIdx.x];
-        const double t = (double)(a.step[0] + 1);
-        consts[threadIdx.x] = Consts{k.beta1, k.rest1, k.beta2, k.rest2, k.eps, k.eta, k.wd, (float)(-1.0 / expm1(t * k.log_beta1)),
-                                     (float)(-1.0 / expm1(t * k.log_beta2))};
+    const int chunk = (int)blockIdx.x;
+    int at = 0;                              // the last tensor that begins at this piece or before
+    for (int end = a.count; end - at > 1;) {
+        const int middle = (at + end) / 2;
+        if (a.t[middle].first_chunk <= chunk) at = middle;
+        else end = middle;
     }
+    const Tensor& t = a.t[at];
+    const Kind& kind = a.kind[t.kind];
+    const int64_t begin = (int64_t)(chunk - t.first_chunk) * CHUNK + threadIdx.x * 8;
+    float x[8], m[8], v[8], g[8];
+    auto load = [&](int64_t i) {
+        load8<X_BF16>(t.X, i, x);
+        load8<G_BF16>(t.G, i, g);
+        load8<false>(t.M, i, m);
+        load8<false>(t.V, i, v);
+    };
+    if (begin + 8 <= t.numel) load(begin);
+    // the bias corrections in 64 bits: 1 - beta^t of a beta near 1 loses most of 24
+    if (threadIdx.x < 2) correction[threadIdx.x] = (float)(-1.0 / expm1((double)(a.step[0] + 1) * (threadIdx.x ? kind.log_beta2 : kind.log_beta1)));
     __syncthreads();
-    int at = 0;
-    for (int chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
-        while (at + 1 < a.count && a.t[at + 1].first_chunk <= chunk) ++at;
-        const Tensor& t = a.t[at];
-        const Consts k = consts[t.kind];
-        const int64_t begin = (int64_t)(chunk - t.first_chunk) * CHUNK;
+    const Consts k{kind.beta1, kind.rest1, kind.beta2, kind.rest2, kind.eps, kind.eta, kind.wd, correction[0], correction[1]};
 #pragma unroll
-        for (int u = 0; u < CHUNK; u += 8 * THREADS) {
-            const int64_t i = begin + u + threadIdx.x * 8;
-            if (i + 8 <= t.numel) {
-                float x[8], m[8], v[8], g[8];
-                load8<X_BF16>(t.X, i, x);
-                load8<G_BF16>(t.G, i, g);
-                load8<false>(t.M, i, m);
-                load8<false>(t.V, i, v);
+    for (int u = 0; u < GROUPS; ++u) {
+        const int64_t i = begin + u * 8 * THREADS;
+        if (i + 8 <= t.numel) {
+            if (u) load(i);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) update(k, x[e], m[e], v[e], g[e]);
-                if (X_BF16)
-                    *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(t.X) + i) =
-                        make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
-                else
-                    store8(reinterpret_cast<float*>(t.X) + i, x);
-                store8(t.M + i, m);
-                store8(t.V + i, v);
-            } else {
-                for (int64_t j = i; j < t.numel && j < i + 8; ++j) {
-                    float x = X_BF16 ? __bfloat162float(reinterpret_cast<__nv_bfloat16*>(t.X)[j]) : reinterpret_cast<float*>(t.X)[j];
-                    const float g = G_BF16 ? __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(t.G)[j]) : reinterpret_cast<const float*>(t.G)[j];
-                    float m = t.M[j], v = t.V[j];
-                    update(k, x, m, v, g);
-                    if (X_BF16) reinterpret_cast<__nv_bfloat16*>(t.X)[j] = __float2bfloat16_rn(x);
-                    else reinterpret_cast<float*>(t.X)[j] = x;
-                    t.M[j] = m; t.V[j] = v;
-                }
+            for (int e = 0; e < 8; ++e) update(k, x[e], m[e], v[e], g[e]);
+            if (X_BF16)
+                *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(t.X) + i) =
+                    make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+            else
+                store8(reinterpret_cast<float*>(t.X) + i, x);
+            store8(t.M + i, m);
+            store8(t.V + i, v);
+        } else {
+            for (int64_t j = i; j < t.numel && j < i + 8; ++j) {
+                float w = X_BF16 ? __bfloat162float(reinterpret_cast<__nv_bfloat16*>(t.X)[j]) : reinterpret_cast<float*>(t.X)[j];
+                const float d = G_BF16 ? __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(t.G)[j]) : reinterpret_cast<const float*>(t.G)[j];
+                float mj = t.M[j], vj = t.V[j];
+                update(k, w, mj, vj, d);
+                if (X_BF16) reinterpret_cast<__nv_bfloat16*>(t.X)[j] = __float2bfloat16_rn(w);
+                else reinterpret_cast<float*>(t.X)[j] = w;
+                t.M[j] = mj; t.V[j] = vj;
             }
         }
     }
@@ -109,7 +114,7 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ 
     __syncthreads();
     if (threadIdx.x == 0) {
         unsigned long long* s = reinterpret_cast<unsigned long long*>(a.step);
-        if (atomicAdd(&s[1], 1ULL) + 1 == (unsigned long long)a.blocks) {
+        if (atomicAdd(&s[1], 1ULL) + 1 == (unsigned long long)gridDim.x) {
             s[1] = 0;
             if (a.last) s[0] += 1;
         }

@@ -39,8 +39,7 @@ struct orthdion_muon_plan {
 struct orthdion_adamw_plan {
     uint32_t magic;
     int64_t numel;
-    double beta1, beta2;
-    float eps, eta, wd;
+    adamw::Kind kind;          // the constants as the kernel takes them
     int32_t x_dtype, g_dtype;
 };
 
@@ -59,9 +58,17 @@ int check_ptr(const void* p) {
 
 // Whether a pointer stands twice among `count`: two matrices of a call that are one would race.
 bool twice(const void* const* p, int32_t count) {
-    std::vector<const void*> v(p, p + count);
-    std::sort(v.begin(), v.end());
-    return std::adjacent_find(v.begin(), v.end()) != v.end();
+    if (count < 2) return false;
+    size_t size = 4;
+    while (size < 2 * (size_t)count) size *= 2;
+    std::vector<const void*> table(size, nullptr);
+    for (int i = 0; i < count; ++i) {
+        size_t at = (reinterpret_cast<uintptr_t>(p[i]) >> 4) * 0x9E3779B97F4A7C15ull >> 20;
+        for (at &= size - 1; table[at]; at = (at + 1) & (size - 1))
+            if (table[at] == p[i]) return true;
+        table[at] = p[i];
+    }
+    return false;
 }
 
 // Two matrices that one launch can serve.  (The bytes of a plan: every field is set by value, padding cleared on creation.)
@@ -455,8 +462,7 @@ int run_adamw(const orthdion_adamw_t* hs, int32_t count, void* const* X, float* 
         for (int i = 0; i < count; ++i) {
             const orthdion_adamw_plan* p = hs[i];
             if ((p->x_dtype == ORTHDION_DTYPE_BF16) + 2 * (p->g_dtype == ORTHDION_DTYPE_BF16) != type) continue;
-            const adamw::Kind k{std::log(p->beta1), std::log(p->beta2), (float)p->beta1, (float)(1.0 - p->beta1), (float)p->beta2, (float)(1.0 - p->beta2),
-                                p->eps, p->eta, p->wd, 0.f};
+            const adamw::Kind& k = p->kind;
             const int64_t chunks = (p->numel + adamw::CHUNK - 1) / adamw::CHUNK;
             if (chunks > (1 << 30)) return ORTHDION_ERR_INVALID_ARG;
             int kind = 0;
@@ -479,8 +485,7 @@ int run_adamw(const orthdion_adamw_t* hs, int32_t count, void* const* X, float* 
     overlap_launches() = true;
     for (size_t i = 0; i < launches.size(); ++i) {
         adamw::Table& t = launches[i];
-        t.blocks = std::min(t.chunks, 8 * sm_count());
-        const dim3 grid((unsigned)t.blocks);
+        const dim3 grid((unsigned)t.chunks);
         cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
         switch (types[i]) {
             case 0: launch(adamw::adamw_kernel<false, false>, grid, adamw::THREADS, 0, 1, prof::S_ADAMW, st, t); break;
@@ -649,7 +654,7 @@ int orthdion_adamw_create(orthdion_adamw_t* out, int64_t numel, double beta1, do
     if (!p) return ORTHDION_ERR_MEMORY;
     p->magic = kAdamWMagic;
     p->numel = numel;
-    p->beta1 = beta1; p->beta2 = beta2; p->eps = eps; p->eta = eta; p->wd = wd;
+    p->kind = adamw::Kind{std::log(beta1), std::log(beta2), (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), eps, eta, wd, 0.f};
     p->x_dtype = p->g_dtype = ORTHDION_DTYPE_BF16;
     *out = p;
     return ORTHDION_OK;
@@ -670,7 +675,7 @@ int orthdion_adamw_set_dtypes(orthdion_adamw_t h, int32_t x_dtype, int32_t g_dty
 
 int orthdion_adamw_set_lr(orthdion_adamw_t h, float eta) {
     if (!valid(h) || !std::isfinite(eta)) return ORTHDION_ERR_INVALID_ARG;
-    h->eta = eta;
+    h->kind.eta = eta;
     return ORTHDION_OK;
 }
 
