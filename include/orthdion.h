@@ -282,7 +282,7 @@ int orthdion_resize_factor(const float* Q_old, int64_t n, int32_t r_old, float* 
  *    results per matrix do not depend on what else is in the call or on what the workspace held. */
 typedef struct orthdion_muon_plan* orthdion_muon_t;
 
-/* Plan for m x n matrices, min(m, n) <= 32768, 0 <= mu < 1.  Defaults: X and G bfloat16, scale 1. */
+/* Plan for m x n matrices, m, n <= 2^18, min(m, n) <= 32768, 0 <= mu < 1.  Defaults: X and G bfloat16, scale 1. */
 int orthdion_muon_create(orthdion_muon_t* out, int64_t m, int64_t n, double mu, float eta, float wd, int32_t nesterov);
 int orthdion_muon_destroy(orthdion_muon_t h);
 int orthdion_muon_set_dtypes(orthdion_muon_t h, int32_t x_dtype, int32_t g_dtype);

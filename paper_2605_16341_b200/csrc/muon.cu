@@ -32,6 +32,7 @@ struct orthdion_muon_plan {
     int32_t nesterov, x_dtype, g_dtype;
     int32_t passes, passes_set;
     int32_t steps;
+    int32_t pairable[2];       // the first two steps, and the last two, as one group
     double eps;
     float abc[kMaxSteps][3];
 };
@@ -88,13 +89,13 @@ struct Groups { int32_t pair_first, pair_last; };
 Groups group_steps(const orthdion_muon_plan* p) {
     const int64_t s = std::min(p->m, p->n), l = std::max(p->m, p->n);
     if (p->passes == 3 && s <= 512) return Groups{0, 0};
-    return Groups{p->steps >= 2, p->steps >= 5 && 4 * l >= 5 * s};
+    return Groups{p->pairable[0], p->steps >= 5 && 4 * l >= 5 * s && p->pairable[1]};
 }
 
 // Tiles and square blocks of the products of one matrix, with tiles of CTA pairs or of single CTAs.
 struct Tiles {
     int32_t sq, x, blocks_sq, blocks_x;
-    int32_t counts() const { return 4 * blocks_sq + 2 * blocks_x; }
+    int32_t counts() const { return 4 * blocks_sq + 2 * blocks_x + sq; }
 };
 template <class SH>
 Tiles tiles_in(int m, int n) {
@@ -105,10 +106,25 @@ Tiles tiles_of(const orthdion_muon_plan* p, bool pair) {
     return pair ? tiles_in<ns::Shape<true>>((int)p->m, (int)p->n) : tiles_in<ns::Shape<false>>((int)p->m, (int)p->n);
 }
 
+// X X^T of few tiles and much depth: units of 16 depth blocks, or up to 32 units, whose sums one of them adds up.  By the matrix's
+// shape alone, so that it has the same bits in whatever call it stands.  A unit begins where a square block of X does in either shape
+// of tile: what it reads is waited for block by block.
+// Orthogonalise, units against whole tiles: 64 x 4096 105 us for 131, 512 x 2048 147 for 152, 512 x 8192 212 for 261, 129 x 70001
+// 369 for 1208; with s = 1024 the sums' way through memory costs what it gains (1024 x 2048 204 for 201, 1024 x 16384 584 for 501).
+struct Splits { int32_t count, depth; };
+Splits splits_of(const orthdion_muon_plan* p) {
+    const int64_t s = std::min(p->m, p->n), blocks = (std::max(p->m, p->n) + 63) / 64;
+    if (s > 512 || blocks < 32) return Splits{1, (int32_t)blocks};
+    constexpr int64_t block = ns::Shape<true>::DEPTH;
+    static_assert(block % ns::Shape<false>::DEPTH == 0 && 16 % block == 0);
+    const int64_t depth = std::max<int64_t>(16, ((blocks + 31) / 32 + block - 1) / block * block);
+    return Splits{(int32_t)((blocks + depth - 1) / depth), (int32_t)depth};
+}
+
 // The scratch of `count` matrices of one plan: byte offsets, strides in elements.
 struct Scratch {
     size_t slot, tile_done, front;             // in the launch's front part, which is cleared: offsets and bytes
-    size_t part, x[2], sq[4], bytes;           // behind it
+    size_t part, split, x[2], sq[4], bytes;    // behind it
     int64_t x_pitch, x_term, x_mat, s_pitch, s_term, s_mat;
 };
 
@@ -124,13 +140,17 @@ Scratch scratch_layout(const orthdion_muon_plan* p, int count) {
     c.front = c.tile_done + align_up((size_t)count * std::max(tiles_of(p, true).counts(), tiles_of(p, false).counts()) * 4, 256);
     size_t off = 0;
     c.part = off; off += align_up((size_t)count * 2 * ns::MAX_PARTS * 8, 1024);
+    c.split = off;
+    const size_t pair_part = (size_t)tiles_of(p, true).sq * ns::Shape<true>::ROWS * ns::Shape<true>::COLS;
+    const size_t single_part = (size_t)tiles_of(p, false).sq * ns::Shape<false>::ROWS * ns::Shape<false>::COLS;
+    off += align_up((size_t)count * (splits_of(p).count - 1) * std::max(pair_part, single_part) * 4, 1024);
     for (int i = 0; i < 2; ++i) {
         c.x[i] = off;
         if (i == 0 || p->steps > 1 + g.pair_first) off += align_up((size_t)count * c.x_mat * 2, 1024);
     }
     for (int i = 0; i < 4; ++i) {
         c.sq[i] = off;
-        if (i < 2 || g.pair_first) off += align_up((size_t)count * c.s_mat * 2, 1024);
+        if (i < 2 || g.pair_first || g.pair_last) off += align_up((size_t)count * c.s_mat * 2, 1024);
     }
     c.bytes = align_up(off, 1024);
     return c;
@@ -306,6 +326,9 @@ void run_launch(const orthdion_muon_t* hs, const Launch& l, void* const* X, floa
         const Tiles tl = tiles_of(p, l.pair);
         c.tiles_sq = tl.sq; c.tiles_x = tl.x; c.blocks_sq = tl.blocks_sq; c.blocks_x = tl.blocks_x; c.counts = tl.counts();
         c.tile_done = reinterpret_cast<uint32_t*>(front + sc.tile_done);
+        const Splits split = splits_of(p);
+        c.splits = split.count; c.split_depth = split.depth;
+        c.part = reinterpret_cast<float*>(base + sc.split);
         c.update = update;
         c.x_bf16 = p->x_dtype == ORTHDION_DTYPE_BF16;
         c.ld_x = p->ld_x;
@@ -351,7 +374,7 @@ void run_launch(const orthdion_muon_t* hs, const Launch& l, void* const* X, floa
     }
 
     int units = 0;                 // of the products with the most tiles
-    for (int k = 0; k < args->classes; ++k) units += std::max(args->c[k].tiles_sq, args->c[k].tiles_x) * args->c[k].count;
+    for (int k = 0; k < args->classes; ++k) units += std::max(args->c[k].tiles_sq * args->c[k].splits, args->c[k].tiles_x) * args->c[k].count;
     const auto kernel = l.pair ? (terms == 2 ? ns::chain_kernel<true, 2> : ns::chain_kernel<true, 1>)
                                : (terms == 2 ? ns::chain_kernel<false, 2> : ns::chain_kernel<false, 1>);
     const int ctas = l.pair ? 2 : 1;
@@ -504,21 +527,24 @@ void default_passes(orthdion_muon_plan* p) {
 }
 
 // Whether singular values in [0, 1] stay within what the images hold (entries up to 255): no value above 8 after any step, no
-// entry of a I + b A + c A^2 above 128.
-bool schedule_ok(int32_t steps, const float* abc) {
-    double top = 1.0;
+// entry of a I + b A + c A^2 above 128, and in a pair of steps none of their product.
+bool schedule_ok(int32_t steps, const float* abc, int32_t (&pairable)[2]) {
+    double top = 1.0, factor[kMaxSteps] = {};
     for (int k = 0; k < steps; ++k) {
         const double a = abc[3 * k], b = abc[3 * k + 1], c = abc[3 * k + 2];
         if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
         if (std::fabs(a) + std::fabs(b) * top * top + std::fabs(c) * top * top * top * top > 128.0) return false;
         double most = 0.0;
         for (int i = 0; i <= 1024; ++i) {
-            const double s = top * i / 1024, s2 = s * s;
-            most = std::max(most, std::fabs(s * (a + b * s2 + c * s2 * s2)));
+            const double s = top * i / 1024, s2 = s * s, f = a + b * s2 + c * s2 * s2;
+            most = std::max(most, std::fabs(s * f));
+            factor[k] = std::max(factor[k], std::fabs(f));
         }
         top = std::max(1e-3, 1.01 * most);
         if (top > 8.0) return false;
     }
+    pairable[0] = steps >= 2 && factor[0] * factor[1] <= 128.0;
+    pairable[1] = steps >= 2 && factor[steps - 2] * factor[steps - 1] <= 128.0;
     return true;
 }
 
@@ -529,7 +555,7 @@ extern "C" {
 int orthdion_muon_create(orthdion_muon_t* out, int64_t m, int64_t n, double mu, float eta, float wd, int32_t nesterov) {
     if (!out) return ORTHDION_ERR_NULL;
     *out = nullptr;
-    if (m < 1 || n < 1 || m > (1 << 24) || n > (1 << 24) || std::min(m, n) > 32768) return ORTHDION_ERR_INVALID_ARG;
+    if (m < 1 || n < 1 || m > (1 << 18) || n > (1 << 18) || std::min(m, n) > 32768) return ORTHDION_ERR_INVALID_ARG;
     if (!(mu >= 0.0 && mu < 1.0) || !std::isfinite(eta) || !std::isfinite(wd) || (nesterov != 0 && nesterov != 1)) return ORTHDION_ERR_INVALID_ARG;
     orthdion_muon_plan* p = new (std::nothrow) orthdion_muon_plan;
     if (!p) return ORTHDION_ERR_MEMORY;
@@ -543,6 +569,7 @@ int orthdion_muon_create(orthdion_muon_t* out, int64_t m, int64_t n, double mu, 
     p->steps = 5;
     p->eps = 1e-7;
     for (int k = 0; k < p->steps; ++k) { p->abc[k][0] = 3.4445f; p->abc[k][1] = -4.7750f; p->abc[k][2] = 2.0315f; }
+    schedule_ok(p->steps, p->abc[0], p->pairable);
     default_passes(p);
     *out = p;
     return ORTHDION_OK;
@@ -585,10 +612,13 @@ int orthdion_muon_set_ld(orthdion_muon_t h, int64_t ld_x, int64_t ld_m, int64_t 
 int orthdion_muon_set_schedule(orthdion_muon_t h, int32_t steps, const float* abc, double eps) {
     if (!valid(h)) return ORTHDION_ERR_INVALID_ARG;
     if (!abc) return ORTHDION_ERR_NULL;
-    if (steps < 1 || steps > kMaxSteps || !(eps >= 0.0 && eps <= 1e30) || !schedule_ok(steps, abc)) return ORTHDION_ERR_INVALID_ARG;
+    if (steps < 1 || steps > kMaxSteps || !(eps >= 0.0 && eps <= 1e30)) return ORTHDION_ERR_INVALID_ARG;
+    int32_t pairable[2];
+    if (!schedule_ok(steps, abc, pairable)) return ORTHDION_ERR_INVALID_ARG;
     std::memset(h->abc, 0, sizeof(h->abc));
     std::memcpy(h->abc, abc, sizeof(float) * 3 * steps);
     h->steps = steps;
+    h->pairable[0] = pairable[0]; h->pairable[1] = pairable[1];
     h->eps = eps;
     return ORTHDION_OK;
 }

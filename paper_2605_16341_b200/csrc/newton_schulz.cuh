@@ -352,11 +352,13 @@ struct Class {
     __half* sq[4];
     int64_t x_pitch, x_term, x_mat, s_pitch, s_term, s_mat;     // in elements
     Slot* slot;
-    uint32_t* tile_done;                      // counts of the square blocks of sq[0] to sq[3] (row by row below the diagonal) and of X
+    uint32_t* tile_done;                      // counts of the square blocks of sq[0] to sq[3] (row by row below the diagonal), of X, of split tiles
     int64_t ld_x;
     int32_t m, n, count, first;               // first: its first matrix in the table
     int32_t steps, pair_first, pair_last;     // steps of the iteration; whether the first and the last two of them are one group
     int32_t tiles_sq, tiles_x;                // tiles of one s x s product, of one product with X
+    int32_t splits, split_depth;              // units that a tile of X X^T is computed as, and the depth blocks of one
+    float* part;                              // [matrix][tile][unit - 1][epilogue warp][column][32 rows]: their sums, but for the first's
     int32_t blocks_sq, blocks_x, counts;      // square blocks of those; counts of one matrix
     int32_t update, x_bf16, x_vec;
     float wc, wd;
@@ -421,7 +423,9 @@ struct Walk {
 };
 struct Unit {
     int cls, mat, stage;
-    int ti, tj, rows, cols, kblocks;          // tile row and column
+    int ti, tj, rows, cols;                   // tile row and column
+    int kb0, kblocks;                         // first depth block, and how many
+    int tile, split, splits;                  // which unit of the tile, of how many
     Op op;
     int a_turn, b_turn;                       // depth block from which on a side is read along its columns
     const CUtensorMap *k_a, *k_b, *mn_a, *mn_b;
@@ -435,7 +439,7 @@ __device__ __forceinline__ bool find_unit(const ChainArgs& g, Walk& w, Unit& u) 
         int units = 0;
         if (w.stage < products(c.steps, c.pair_first, c.pair_last)) {
             u.op = op_of(c, w.stage);
-            units = (u.op.kind == OP_APPLY ? c.tiles_x : c.tiles_sq) * c.count;
+            units = (u.op.kind == OP_APPLY ? c.tiles_x : c.tiles_sq) * c.count * (u.op.kind == OP_GRAM ? c.splits : 1);
         }
         if (w.unit < w.base + units) break;
         w.base += units;
@@ -445,11 +449,21 @@ __device__ __forceinline__ bool find_unit(const ChainArgs& g, Walk& w, Unit& u) 
     const bool apply = u.op.kind == OP_APPLY;
     const int s = min(c.m, c.n), l = max(c.m, c.n), tiles = apply ? c.tiles_x : c.tiles_sq;
     int t = w.unit - w.base;
+    u.split = 0; u.splits = 1; u.kb0 = 0;
+    u.kblocks = ((u.op.kind == OP_GRAM ? l : s) + 63) / 64;
+    if (u.op.kind == OP_GRAM && c.splits > 1) {
+        // the first, which adds the others' sums to its own, comes last
+        u.splits = c.splits;
+        u.split = c.splits - 1 - t % c.splits;
+        t /= c.splits;
+        u.kb0 = u.split * c.split_depth;
+        u.kblocks = min(c.split_depth, u.kblocks - u.kb0);
+    }
     u.cls = w.cls; u.stage = w.stage;
     u.mat = t / tiles;
     t -= u.mat * tiles;
     u.rows = apply ? c.m : s; u.cols = apply ? c.n : s;
-    u.kblocks = ((u.op.kind == OP_GRAM ? l : s) + 63) / 64;
+    u.tile = t;
     if (!apply) {
         u.ti = (int)((sqrtf((8.f / SH::Q) * t + 1.f) - 1.f) * 0.5f);
         while (SH::before(u.ti) > t) --u.ti;
@@ -570,6 +584,50 @@ __device__ __forceinline__ bool wait_count(const uint32_t* p, uint32_t want, vol
 // Units of a matrix's products before product `stage`, which begins group `group` or belongs to it.
 __device__ __forceinline__ uint32_t units_before(const Class& c, int stage, int group) {
     return (uint32_t)((stage - group) * c.tiles_sq + group * c.tiles_x);
+}
+
+// A tile of X X^T in several units.  All but the first store their sums, column by column, and raise the tile's count; the first waits
+// for them (they come before it in every walk) and adds them to its own in tensor memory, always in the same order.
+template <class SH, int NC>
+__device__ __noinline__ bool split_epilogue(const Class& c, const Unit& u, uint32_t d, bool mine, int at, int lane, volatile int* abort_flag) {
+    constexpr int WARP = NC * 32, TILE = SH::ARRIVALS * WARP;
+    float* part = c.part + ((int64_t)u.mat * c.tiles_sq + u.tile) * (u.splits - 1) * TILE + at * WARP + lane;
+    uint32_t* done = c.tile_done + (int64_t)u.mat * c.counts + 4 * c.blocks_sq + 2 * c.blocks_x + u.tile;
+    if (u.split) {
+        if (mine) {
+            part += (u.split - 1) * TILE;
+#pragma unroll 1
+            for (int q = 0; q < NC; q += 16) {
+                uint32_t x[16];
+                tmem_ld16(d + q, x);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) __stcg(part + (q + e) * 32, __uint_as_float(x[e]));
+            }
+        }
+        __syncwarp();
+        if (lane == 0) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(done) : "memory");
+        return true;
+    }
+    if (!__all_sync(0xffffffffu, wait_count(done, SH::ARRIVALS * (uint32_t)((u.splits - 1) * (u.op.group + 1)), abort_flag))) return false;
+    if (mine) {
+#pragma unroll 1
+        for (int q = 0; q < NC; q += 16) {
+            uint32_t x[16];
+            float v[16];
+            tmem_ld16(d + q, x);
+            tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(x[e]);
+#pragma unroll 2
+            for (int p = 0; p < u.splits - 1; ++p)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[e] += __ldcg(part + p * TILE + (q + e) * 32);
+            tmem_st16(d + q, v);
+        }
+        tmem_st_wait();
+    }
+    return true;
 }
 
 // The rows of one warp (row_w + lane) and NC columns from col_w of a result in tensor memory at d -> image, through 4 KB of shared memory:
@@ -855,7 +913,7 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
                 bool there = true;
                 if (k < kblocks) {
                     int per_a, per_b;
-                    const int at_a = place_of<SH>(c, a, k, per_a), at_b = place_of<SH>(c, b, k, per_b);
+                    const int at_a = place_of<SH>(c, a, u.kb0 + k, per_a), at_b = place_of<SH>(c, b, u.kb0 + k, per_b);
                     const uint32_t x = load_relaxed(counts + at_a), y = load_relaxed(counts + at_b);
                     there = (int32_t)(x - writes_a * per_a) >= 0 && (int32_t)(y - writes_b * per_b) >= 0;
                 }
@@ -886,7 +944,7 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
             bool ok = true;
             while (ok && mbar_wait(ufull0 + 8 * e, eph, abort_flag)) {
                 const Unit& u = *unit_at(e);
-                const int kblocks = u.kblocks, mat = u.mat, a_turn = u.a_turn, b_turn = u.b_turn;
+                const int kblocks = u.kblocks, kb0 = u.kb0, mat = u.mat, a_turn = u.a_turn, b_turn = u.b_turn;
                 if (!kblocks) break;
                 const CUtensorMap *ka = u.k_a, *kb_ = u.k_b, *ma = u.mn_a, *mb = u.mn_b;
                 const int ar = u.ti * SH::ROWS + crank * 128, br = u.tj * SH::COLS + crank * SH::B_ROWS;
@@ -906,10 +964,10 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
                         const uint32_t fb = full_ld + 8 * s, dst = base + s * STAGE;
                         if (PAIR) mbar_arrive_expect_tx_remote(fb, STAGE);
                         else mbar_arrive_expect_tx(fb, STAGE);
-                        if (a_mn) tma_load_mn<PAIR>(dst, ma, kb * 64, ar / 64, mat, fb);
-                        else tma_load_k<PAIR>(dst, ka, kb * 64, ar, mat, fb);
-                        if (b_mn) tma_load_mn<PAIR>(dst + A_BYTES, mb, kb * 64, br / 64, mat, fb);
-                        else tma_load_k<PAIR>(dst + A_BYTES, kb_, kb * 64, br, mat, fb);
+                        if (a_mn) tma_load_mn<PAIR>(dst, ma, (kb0 + kb) * 64, ar / 64, mat, fb);
+                        else tma_load_k<PAIR>(dst, ka, (kb0 + kb) * 64, ar, mat, fb);
+                        if (b_mn) tma_load_mn<PAIR>(dst + A_BYTES, mb, (kb0 + kb) * 64, br / 64, mat, fb);
+                        else tma_load_k<PAIR>(dst + A_BYTES, kb_, (kb0 + kb) * 64, br, mat, fb);
                         if (++s == NS) { s = 0; ph ^= 1; }
                     }
                 }
@@ -1029,7 +1087,13 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
             // In a 256 x 256 tile on the diagonal the 128 x 128 block above it is the one below, mirrored, as it is between tiles of the other
             // shape: Q A rounds another way above the diagonal than below, and a matrix gets the same bits in whatever call it stands.
             const bool on_diagonal = PAIR && !apply && u.ti == u.tj, above = on_diagonal && crank == 0 && half == 1;
-            if (row_w < u.rows && col_w < u.cols && !above) {
+            bool mine = row_w < u.rows && col_w < u.cols && !above;
+            if (u.splits > 1) {
+                ok = split_epilogue<SH, NC>(c, u, d, mine, crank * 8 + warp - 4, lane, abort_flag);
+                if (!ok) break;
+                mine = mine && !u.split;
+            }
+            if (mine) {
                 float alpha = 1.f / UNIT;
                 // the images hold UNIT times the value, the first one of X divided by sigma
                 if (u.op.group == 0 && u.op.kind == OP_GRAM) { const float sg = __ldcg(&slot->sigma); alpha *= sg * sg; }
@@ -1059,7 +1123,7 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
             if (u.op.out >= 0) {
                 // every lane's stores before the counts (which release them, by way of lane 0)
                 __syncwarp();
-                if (lane == 0) {
+                if (lane == 0 && !u.split) {
                     const int bj = u.tj / SH::Q;
                     const int place = u.op.out < 4 ? u.op.out * c.blocks_sq + u.ti * (u.ti + 1) / 2 + bj
                                                    : 4 * c.blocks_sq + (u.op.out - 4) * c.blocks_x + u.ti * SH::blocks(c.n) + bj;

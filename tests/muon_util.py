@@ -4,8 +4,9 @@ The bound of the orthogonalisation counts what the library rounds (see `orthogon
 to u relative to each entry, every sum by gamma relative to the sum of its terms' magnitudes.  A rounding is off by at most half a
 step: fp16 2^-11, bf16 2^-8.  Two-term operands are off by 2^-22 and their product drops a term of 2^-22.  An addition in tensor
 memory truncates: 2^-23 each; one product of depth K there is K/16 of them (one-term operands), or 12 for each 64 deep and one rounded
-addition (2^-24) for each 64.  Errors in X pass a step with its Lipschitz constant, max |p'| over the singular values'
-range (the map of singular values is odd, so this bounds the matrix map in the Frobenius norm).
+addition (2^-24) for each 64; up to 32 partial sums of a long depth are added up (2^-24 each).  Errors in X pass a step with its
+Lipschitz constant, max |p'| over the singular values' range (the map of singular values is odd, so this bounds the matrix map in the
+Frobenius norm).
 """
 import torch
 
@@ -26,7 +27,7 @@ def orthogonalise(B, schedule, eps=1e-7):
     return X
 
 
-def bound(B, schedule, passes, x_dtype, eps=1e-7, exact_input=False):
+def bound(B, schedule, passes, x_dtype, eps=1e-7, exact_input=False, pairs=(True, True)):
     """Largest ||O - exact||_F / ||exact||_F that the roundings above can add up to."""
     X = B.double()
     if X.shape[0] > X.shape[1]:
@@ -38,7 +39,7 @@ def bound(B, schedule, passes, x_dtype, eps=1e-7, exact_input=False):
 
     def gamma(depth):
         blocks = -(-depth // 64)
-        return drop + (blocks * 4 * 2.0 ** -23 if passes == 1 else 12 * 2.0 ** -23 + blocks * 2.0 ** -24)
+        return drop + 32 * 2.0 ** -24 + (blocks * 4 * 2.0 ** -23 if passes == 1 else 12 * 2.0 ** -23 + blocks * 2.0 ** -24)
 
     fro = lambda t: torch.linalg.matrix_norm(t).item()  # noqa: E731
 
@@ -55,9 +56,10 @@ def bound(B, schedule, passes, x_dtype, eps=1e-7, exact_input=False):
     # steps between two roundings of X: two in front, and two at the end of five or more where the matrix is longer than wide;
     # one by one where a small matrix has two-term operands
     singles = passes == 3 and s <= 512
-    k, pair_last = 0, len(schedule) >= 5 and 4 * l >= 5 * s and not singles
+    # (`pairs`: whether the factors of the first two steps, and of the last two, fit the images together)
+    k, pair_last = 0, pairs[1] and len(schedule) >= 5 and 4 * l >= 5 * s and not singles
     while k < len(schedule):
-        steps = schedule[k:k + (2 if (k == 0 and not singles) or (pair_last and len(schedule) - k == 2) else 1)]
+        steps = schedule[k:k + (2 if (k == 0 and pairs[0] and not singles) or (pair_last and len(schedule) - k == 2) else 1)]
         A = X @ X.T
         dA = u * fro(A) + gamma(l) * fro(X) ** 2 + 2.0 ** -22 * fro(A)
         P = dP = None

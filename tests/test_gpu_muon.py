@@ -171,6 +171,56 @@ def test_large_tiles(m, n, count, x):
         assert torch.equal(O, orth(G, x))
 
 
+@pytest.mark.parametrize("x", [BF16, F32])
+@pytest.mark.parametrize("m,n,count", [(64, 2048, 1), (7, 8191, 2), (5000, 100, 1), (300, 2500, 20), (1024, 2100, 2), (1025, 2100, 1),
+                                       (3, 200_003, 1), (70_001, 129, 1)])
+def test_long_matrices(m, n, count, x):
+    """Few rows (or columns) and a long other side, whose first product is computed in parts: against the definition, repeatably, and
+    with the same bits in a call of several."""
+    hs = [plan(m, n, x=x)] * count
+    Gs = [gradient(("spikes", "noise")[i % 2], m, n, i, BF16) for i in range(count)]
+    outs = []
+    for _ in range(2):
+        Os = [torch.full((m, n), float("nan"), dtype=x, device="cuda") for _ in range(count)]
+        ws = workspace(hs)
+        od.orthdion_orthogonalize_grouped(od.MuonTable(hs, Os, None, Gs), ws)
+        assert od.orthdion_muon_last_status(count, ws) == [0] * count
+        outs.append(Os)
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
+    for G, O in list(zip(Gs, outs[0]))[:3]:
+        ref = orthogonalise(G if m <= n else G.T, [FAST] * 5)
+        passes = 3 if x == F32 else 1
+        assert rel(O, ref if m <= n else ref.T) <= STATED[passes]
+        assert torch.equal(O, orth(G, x))
+
+
+def test_more_plans_than_one_launch_takes():
+    """Nine plans, both pass counts, in one call: several launches, which use the same scratch one after the other."""
+    shapes = [(64 + 8 * k, 200) for k in range(9)] * 2
+    hs = [plan(m, n, x=(BF16, F32)[i % 2]) for i, (m, n) in enumerate(shapes)]
+    Gs = [gradient("spikes", m, n, i, BF16) for i, (m, n) in enumerate(shapes)]
+    Xs = [(0.02 * torch.randn(m, n, device="cuda")).to((BF16, F32)[i % 2]) for i, (m, n) in enumerate(shapes)]
+    Ms = [0.1 * torch.randn(m, n, device="cuda") for m, n in shapes]
+    single = [(X.clone(), M.clone()) for X, M in zip(Xs, Ms)]
+    ws = workspace(hs)
+    od.orthdion_muon_step_grouped(od.MuonTable(hs, Xs, Ms, Gs), ws)
+    assert od.orthdion_muon_last_status(len(hs), ws) == [0] * len(hs)
+    for h, (X, M), G, gx, gm in zip(hs, single, Gs, Xs, Ms):
+        od.orthdion_muon_step(h, X, M, G, workspace([h], 0))
+        assert torch.equal(X, gx) and torch.equal(M, gm)
+
+
+@pytest.mark.parametrize("passes", [1, 3])
+@pytest.mark.parametrize("tail", [[], [FAST, FAST]], ids=["three", "five"])
+def test_steep_schedules(tail, passes):
+    """Two steps whose factors together (20 and 7) are beyond what an image holds are taken one by one, in front of a pair or not."""
+    steep = [(20.0, -50.0, 32.0), (7.0, -0.9, 0.024), (0.125, 0.0, 0.0)] + tail
+    for m, n in ((600, 800), (100, 260)):
+        G = gradient("spikes", m, n, 2, BF16)
+        got = orth(G, F32, steep, passes=passes)
+        assert rel(got, orthogonalise(G, steep)) <= bound(G, steep, passes, F32, exact_input=True, pairs=(False, True))
+
+
 def test_grouped_orthogonalise_and_in_place():
     shapes = [(64, 200), (200, 64), (64, 200)]
     hs = [plan(m, n) for m, n in shapes]

@@ -20,12 +20,12 @@ def muon(L, m=64, n=48, mu=0.95, eta=0.02, wd=0.1, nesterov=1):
 
 def test_muon_create_refuses(L):
     nan = float("nan")
-    for kw in (dict(m=0), dict(n=0), dict(m=-1), dict(m=1 << 25), dict(m=40000, n=40000), dict(mu=1.0), dict(mu=-0.1), dict(mu=nan), dict(eta=nan),
+    for kw in (dict(m=0), dict(n=0), dict(m=-1), dict(m=(1 << 18) + 1), dict(m=40000, n=40000), dict(mu=1.0), dict(mu=-0.1), dict(mu=nan), dict(eta=nan),
                dict(wd=float("inf")), dict(nesterov=2)):
         rc, h = muon(L, **kw)
         assert rc == -1 and not h.value, kw
     assert L.orthdion_muon_create(None, 4, 4, 0.9, 0.1, 0.0, 1) == -3
-    rc, h = muon(L, m=1, n=1 << 24)
+    rc, h = muon(L, m=1, n=1 << 18)
     assert rc == 0 and L.orthdion_muon_destroy(h) == 0 and L.orthdion_muon_destroy(h) == -1
     assert L.orthdion_muon_destroy(None) == -1
 
