@@ -275,10 +275,11 @@ int orthdion_resize_factor(const float* Q_old, int64_t n, int32_t r_old, float* 
  *    apart than n entries (orthdion_muon_set_ld); what lies between them is not touched.
  *  - Products run on the tensor cores in fp16 with fp32 sums.  passes = 1: one product of 11-bit operands, an error of
  *    1e-3 to 4e-3 of the result; 3: two-term operands of 22 bits, three products, about 2e-6.  Default: 1 where X is
- *    bfloat16 (its rounding is 1.7e-3), 3 where X is float32.  The norm is summed in 64 bits.
+ *    bfloat16 (its rounding is 1.7e-3), 3 where X is float32.  The norm is summed in 64 bits (squares eight at a time in 32).
  *  - A matrix of zeros has the result zero.  Where ||B||_F is below 1e-4 * eps the result, which is then small too, loses bits.
  *  - A matrix whose B holds Inf or NaN (or a sum of squares beyond them) gets ORTHDION_STATUS_NONFINITE and keeps X and M (O).
- *  - No matrix may stand twice in a call (ORTHDION_ERR_INVALID_ARG).  Matrices of equal plans share launches;
+ *  - No matrix may stand twice in a call (ORTHDION_ERR_INVALID_ARG), and but for O = G no buffer may overlap another that is
+ *    written.  Calls that may run at the same time need a workspace each.  Matrices of equal plans share launches;
  *    results per matrix do not depend on what else is in the call or on what the workspace held. */
 typedef struct orthdion_muon_plan* orthdion_muon_t;
 
@@ -320,7 +321,8 @@ int orthdion_muon_last_status(int32_t count, const void* workspace, void* stream
  * Tensors are contiguous, of any length, 16-byte aligned; X and G float32 or bfloat16, m and v float32 (zeros before the first
  * step); X, m, v in place.  step: DEVICE pointer to two int64, [0] the steps taken so far, which the call raises by one when it
  * has read it (so a captured and replayed call goes on counting), [1] zero, the library's.  All tensors of a call are at the
- * same step; a tensor may stand in it once.  No workspace. */
+ * same step; a tensor may stand in it once (ORTHDION_ERR_INVALID_ARG), and no buffer may overlap another that is written.
+ * No workspace. */
 typedef struct orthdion_adamw_plan* orthdion_adamw_t;
 
 /* 1 <= numel <= 2^40, 0 <= beta < 1, eps >= 0.  Defaults: X and G bfloat16. */
@@ -341,7 +343,8 @@ int64_t orthdion_launch_count(void);
  * the recorded events and returns, per stage s < orthdion_stage_count(), the summed device time
  * ms[s] in milliseconds and the number of launches.  Stages are the kernels of the step: the
  * packers, Y = B*Q_prev, Gram, Cholesky+inverse, apply (the QR of the left-factor and normalisation steps),
- * R = B^T*P, ColNorm and the fused feedback/update pass.
+ * R = B^T*P, ColNorm and the fused feedback/update pass; of the full-rank steps the buffer (norm, momentum, image) and all
+ * products together; and the AdamW step.
  * Not thread-safe; meant for benchmarks. */
 int orthdion_profile_begin(int32_t max_launches);
 int orthdion_profile_end(int32_t n_stages, double* ms, int64_t* launches);

@@ -356,12 +356,12 @@ def orthdion_muon_create(m, n, mu, eta, wd, nesterov=True) -> int:
 
 def orthdion_muon_destroy(h):
     _check(lib().orthdion_muon_destroy(h), "orthdion_muon_destroy")
-    _plans.pop(h, None)
+    _plan_changed(h, None)
 
 
 def orthdion_muon_set_dtypes(h, x_dtype, g_dtype):
     _check(lib().orthdion_muon_set_dtypes(h, _dt(x_dtype), _dt(g_dtype)), "orthdion_muon_set_dtypes")
-    _plans[h].dtypes = [x_dtype, g_dtype]
+    _plan_changed(h, dtypes=[x_dtype, g_dtype])
 
 
 def orthdion_muon_set_lr(h, eta):
@@ -375,7 +375,7 @@ def orthdion_muon_set_scale(h, scale):
 def orthdion_muon_set_ld(h, ld_x, ld_m, ld_g):
     """Entries from one row to the next of X (or the result), M and G, for matrices that are columns of wider ones."""
     _check(lib().orthdion_muon_set_ld(h, ld_x, ld_m, ld_g), "orthdion_muon_set_ld")
-    _plans[h].ld = [ld_x, ld_m, ld_g]
+    _plan_changed(h, ld=[ld_x, ld_m, ld_g])
 
 
 def orthdion_muon_set_schedule(h, coefficients, eps=1e-7):
@@ -407,6 +407,42 @@ class _Plan:
 
 
 _plans: dict = {}
+_changes = 0          # of plans so far: a table whose plans may have changed since it was built checks its tensors again
+
+
+def _plan_changed(h, *gone, **fields):
+    global _changes
+    _changes += 1
+    if gone:
+        _plans.pop(h, None)
+    for name, value in fields.items():
+        setattr(_plans[h], name, value)
+
+
+def _workspace(t):
+    return _here(t, "workspace"), t.numel() * t.element_size()
+
+
+def _here(t, name) -> int:
+    p = _dev_ptr(t, name)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current device")
+    return p
+
+
+class _Table:
+    """Host arrays of device pointers; before a call: still the plans' shapes and types, still the current device."""
+
+    def _check_now(self):
+        if self._seen != _changes:
+            self._pointers()
+            self._seen = _changes
+        if self._device != torch.cuda.current_device():
+            raise ValueError("the table's tensors are not on the current device")
+
+    def _built(self):
+        self._pointers()
+        self._seen, self._device = _changes, torch.cuda.current_device()
 
 
 def _matrix_ptr(t, name, h, ld, dtype, device):
@@ -424,9 +460,10 @@ def _matrix_ptr(t, name, h, ld, dtype, device):
 
 def _muon_ptrs(h, X, M, G):
     """Pointers of one matrix's tensors (M None: an orthogonalisation)."""
-    p, dev = _plans.get(h), torch.device("cuda", torch.cuda.current_device())
-    if p is None:
+    p = _plans.get(h)
+    if p is None or p.ld is None:
         raise OrthDionError(-1, "no such plan")
+    dev = torch.device("cuda", torch.cuda.current_device())
     return (_matrix_ptr(X, "X", h, p.ld[0], p.dtypes[0], dev),
             None if M is None else _matrix_ptr(M, "M", h, p.ld[1], torch.float32, dev),
             _matrix_ptr(G, "G", h, p.ld[2], p.dtypes[1], dev))
@@ -435,20 +472,16 @@ def _muon_ptrs(h, X, M, G):
 def orthdion_orthogonalize(h, G, O, workspace, stream=None):
     """O = the Newton-Schulz orthogonalisation of G.  O has the plan's x_dtype, G its g_dtype."""
     o, _, g = _muon_ptrs(h, O, None, G)
-    _check(lib().orthdion_orthogonalize(h, g, o, _dev_ptr(workspace, "workspace"),
-                                        workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
-           "orthdion_orthogonalize")
+    _check(lib().orthdion_orthogonalize(h, g, o, *_workspace(workspace), _stream_ptr(stream)), "orthdion_orthogonalize")
 
 
 def orthdion_muon_step(h, X, M, G, workspace, stream=None):
     """One Muon step of one matrix; X and M are updated in place."""
     x, m, g = _muon_ptrs(h, X, M, G)
-    _check(lib().orthdion_muon_step(h, x, m, g, _dev_ptr(workspace, "workspace"),
-                                    workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
-           "orthdion_muon_step")
+    _check(lib().orthdion_muon_step(h, x, m, g, *_workspace(workspace), _stream_ptr(stream)), "orthdion_muon_step")
 
 
-class MuonTable:
+class MuonTable(_Table):
     """Host arrays of device pointers for the grouped full-rank calls, built once and reused.  Ms None: a table for
     orthdion_orthogonalize_grouped, Xs the results."""
 
@@ -456,29 +489,34 @@ class MuonTable:
         n = len(hs)
         if not (n and len(Xs) == len(Gs) == n and (Ms is None or len(Ms) == n)):
             raise ValueError("one plan, X, M and G per matrix")
+        self.n, self._keep = n, (list(hs), list(Xs), None if Ms is None else list(Ms), list(Gs))
+        self._built()
+
+    def _pointers(self):
+        hs, Xs, Ms, Gs = self._keep
         ptrs = [_muon_ptrs(h, Xs[i], None if Ms is None else Ms[i], Gs[i]) for i, h in enumerate(hs)]
-        arr = ctypes.c_void_p * n
-        self.n, self.hs = n, arr(*hs)
-        self.X, self.G = arr(*[p[0] for p in ptrs]), arr(*[p[2] for p in ptrs])
+        arr = ctypes.c_void_p * self.n
+        self.hs, self.X, self.G = arr(*hs), arr(*[p[0] for p in ptrs]), arr(*[p[2] for p in ptrs])
         self.M = None if Ms is None else arr(*[p[1] for p in ptrs])
-        self._keep = (list(Xs), None if Ms is None else list(Ms), list(Gs))
 
 
 def orthdion_orthogonalize_grouped(table: MuonTable, workspace, stream=None):
-    _check(lib().orthdion_orthogonalize_grouped(table.hs, table.n, table.G, table.X, _dev_ptr(workspace, "workspace"),
-                                                workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
+    table._check_now()
+    _check(lib().orthdion_orthogonalize_grouped(table.hs, table.n, table.G, table.X, *_workspace(workspace), _stream_ptr(stream)),
            "orthdion_orthogonalize_grouped")
 
 
 def orthdion_muon_step_grouped(table: MuonTable, workspace, stream=None):
-    _check(lib().orthdion_muon_step_grouped(table.hs, table.n, table.X, table.M, table.G, _dev_ptr(workspace, "workspace"),
-                                            workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
+    table._check_now()
+    _check(lib().orthdion_muon_step_grouped(table.hs, table.n, table.X, table.M, table.G, *_workspace(workspace), _stream_ptr(stream)),
            "orthdion_muon_step_grouped")
 
 
 def orthdion_muon_last_status(count, workspace, stream=None):
     flags = (ctypes.c_int32 * count)()
-    _check(lib().orthdion_muon_last_status(count, _dev_ptr(workspace, "workspace"), _stream_ptr(stream), flags),
+    if workspace.numel() * workspace.element_size() < 4 * count:
+        raise OrthDionError(-4, "orthdion_muon_last_status")
+    _check(lib().orthdion_muon_last_status(count, _here(workspace, "workspace"), _stream_ptr(stream), flags),
            "orthdion_muon_last_status")
     return list(flags)
 
@@ -492,30 +530,35 @@ def orthdion_adamw_create(numel, beta1, beta2, eps, eta, wd) -> int:
 
 def orthdion_adamw_destroy(h):
     _check(lib().orthdion_adamw_destroy(h), "orthdion_adamw_destroy")
-    _plans.pop(h, None)
+    _plan_changed(h, None)
 
 
 def orthdion_adamw_set_dtypes(h, x_dtype, g_dtype):
     _check(lib().orthdion_adamw_set_dtypes(h, _dt(x_dtype), _dt(g_dtype)), "orthdion_adamw_set_dtypes")
-    _plans[h].dtypes = [x_dtype, g_dtype]
+    _plan_changed(h, dtypes=[x_dtype, g_dtype])
 
 
 def orthdion_adamw_set_lr(h, eta):
     _check(lib().orthdion_adamw_set_lr(h, eta), "orthdion_adamw_set_lr")
 
 
-class AdamWTable:
+class AdamWTable(_Table):
     """Host arrays of device pointers for orthdion_adamw_step_grouped, built once and reused."""
 
     def __init__(self, hs, Xs, Ms, Vs, Gs):
         n = len(hs)
         if not (n and len(Xs) == len(Ms) == len(Vs) == len(Gs) == n):
             raise ValueError("one plan, X, M, V and G per tensor")
+        self.n, self._keep = n, (list(hs), list(Xs), list(Ms), list(Vs), list(Gs))
+        self._built()
+
+    def _pointers(self):
+        hs, Xs, Ms, Vs, Gs = self._keep
         dev = torch.device("cuda", torch.cuda.current_device())
 
         def ptr(t, name, h, dtype):
             p = _plans.get(h)
-            if p is None:
+            if p is None or p.ld is not None:
                 raise OrthDionError(-1, f"{name}: no such plan")
             if not t.is_cuda or t.device != dev:
                 raise ValueError(f"{name} must be a CUDA tensor on the current device")
@@ -523,24 +566,24 @@ class AdamWTable:
                 raise ValueError(f"{name}: the plan has {p.m} entries of {dtype}, got {t.numel()} of {t.dtype}")
             return _dev_ptr(t, name)
 
-        arr = ctypes.c_void_p * n
+        arr = ctypes.c_void_p * self.n
         xt, gt = [[_plans[h].dtypes[k] if h in _plans else None for h in hs] for k in (0, 1)]
-        self.n, self.hs = n, arr(*hs)
+        self.hs = arr(*hs)
         self.X = arr(*[ptr(t, "X", h, d) for t, h, d in zip(Xs, hs, xt)])
         self.M = arr(*[ptr(t, "M", h, torch.float32) for t, h in zip(Ms, hs)])
         self.V = arr(*[ptr(t, "V", h, torch.float32) for t, h in zip(Vs, hs)])
         self.G = arr(*[ptr(t, "G", h, d) for t, h, d in zip(Gs, hs, gt)])
-        self._keep = (list(Xs), list(Ms), list(Vs), list(Gs))
 
 
 def _step_ptr(step) -> int:
     if step.dtype != torch.int64 or step.numel() != 2:
         raise ValueError("step: two int64, the steps taken and a zero")
-    return _dev_ptr(step, "step")
+    return _here(step, "step")
 
 
 def orthdion_adamw_step_grouped(table: AdamWTable, step, stream=None):
     """One AdamW step of every tensor of the table; step: CUDA tensor of two int64, [steps taken, 0]."""
+    table._check_now()
     _check(lib().orthdion_adamw_step_grouped(table.hs, table.n, table.X, table.M, table.V, table.G, _step_ptr(step),
                                              _stream_ptr(stream)), "orthdion_adamw_step_grouped")
 

@@ -9,7 +9,7 @@
 //
 // Sums are fp32, in tensor memory.  The tensor core truncates as it adds, which lowers a long sum of squares by about 5e-9 of it
 // per term: two-plane products are summed over 64 terms at a time there, the small products first, and beyond that by the epilogue, in
-// registers (256 x 512 in fp32: error of the result 1.3e-5 with 256 terms at a time, 3.1e-6 with 64; the plain form in fp32 has 2e-6).
+// registers (256 x 512 in fp32: error of the result 1.3e-5 with 256 terms at a time, 2e-6 with 64, which is what fp32 products have).
 #pragma once
 #include <cuda_fp16.h>
 
@@ -69,8 +69,6 @@ struct BufferArgs {
     PrepArgs c[MAX_CLASSES];
 };
 
-// 8 entries of G and M from (row, col) as they lie in memory: one after the other, or 32 columns apart where rows start on no 16-byte boundary (the
-// lanes of a warp then take neighbouring ones); zeros beyond the last column.
 // What a buffer kernel is made for.  VEC: rows start on 16-byte boundaries, and have whole vectors.  MOMENTUM: B comes from G and M, else from G alone.
 template <bool VEC_, bool G_BF16_, bool MOMENTUM_>
 struct Form { static constexpr bool VEC = VEC_, G_BF16 = G_BF16_, MOMENTUM = MOMENTUM_; };
@@ -78,6 +76,8 @@ template <class F>
 struct Raw {
     uint4 g[F::G_BF16 ? 1 : 2], m[F::MOMENTUM ? 2 : 1];
 };
+// 8 entries of G and M from (row, col) as they lie in memory: one after the other, or 32 columns apart where rows start on no 16-byte boundary (the
+// lanes of a warp then take neighbouring ones); zeros beyond the last column.
 template <class F>
 __device__ __forceinline__ void load_raw(const Mat& w, const PrepArgs& a, int64_t row, int64_t col, Raw<F>& r) {
     const int64_t gi = row * a.ld_g + col, mi = row * a.ld_m + col;
@@ -234,7 +234,7 @@ __device__ __forceinline__ void write_segment(const Mat& w, const PrepArgs& a, i
 // [128, 256) (a gradient in bf16 is then held exactly; what is left of the normalisation, sigma, goes into the factors of the first products), and
 // the updated momentum.  A matrix whose norm is not finite keeps its momentum.  The second look at B finds most of it in L2: a team
 // works on one matrix at a time and goes back over it the way it came.  (As two launches, norms of all matrices and then images, the seven
-// matrices of a layer of a 1.1B model took 225 us, 18 bytes an entry at 4.1 TB/s.)  The squares are summed in 64 bits.
+// matrices of a layer of a 1.1B model took 225 us, 18 bytes an entry at 4.1 TB/s, for 187 now.)
 template <class FORM>
 __global__ void __launch_bounds__(BUFFER_THREADS, BUFFER_BLOCKS) buffer_kernel(const __grid_constant__ Table t, const __grid_constant__ BufferArgs g) {
     __shared__ double red[BUFFER_THREADS / 32];
@@ -250,6 +250,7 @@ __global__ void __launch_bounds__(BUFFER_THREADS, BUFFER_BLOCKS) buffer_kernel(c
         Slot* slot = a.slot + mat;
         double* part = a.part + (int64_t)mat * (2 * MAX_PARTS);
         double sum = 0.0;
+        int gave_up = 0;
         // Once with squares in 32 bits, eight at a time; where the sum says that some overflowed or most of it vanished, all in 64.
         for (int wide = 0; wide < 2; ++wide) {
             for (int seg = rank; seg < a.parts; seg += g.team) {
@@ -268,12 +269,13 @@ __global__ void __launch_bounds__(BUFFER_THREADS, BUFFER_BLOCKS) buffer_kernel(c
                 failed = (int32_t)(v - want) < 0;
             }
             __syncthreads();
+            gave_up = failed;                // (before the next barrier: thread 0 may be at the next matrix soon after it)
             sum = 0.0;
 #pragma unroll
             for (int i = 0; i < MAX_PARTS; i += BUFFER_THREADS)
                 if (i + (int)threadIdx.x < a.parts) sum += __ldcg(part + wide * MAX_PARTS + i + threadIdx.x);
             sum = block_sum(sum, red);
-            if (failed || (sum >= 1e-20 && sum <= 1.7e308)) break;
+            if (gave_up || (sum >= 1e-20 && sum <= 1.7e308)) break;
         }
         const double norm = sqrt(sum);
         const bool finite = norm <= 1.7e308;
@@ -282,12 +284,12 @@ __global__ void __launch_bounds__(BUFFER_THREADS, BUFFER_BLOCKS) buffer_kernel(c
         const int p2 = finite && norm > 0.0 ? 8 - e : 0;
         // (the power itself may be beyond fp32, so two factors)
         const float f1 = ldexpf(1.f, p2 / 2), f2 = ldexpf(1.f, p2 - p2 / 2);
-        if (threadIdx.x == 0 && (rank == 0 || failed)) {
+        if (threadIdx.x == 0 && (rank == 0 || gave_up)) {
             slot->sigma = finite && norm > 0.0 ? (float)((double)UNIT / ldexp(norm + a.eps, p2)) : 0.f;
-            slot->status = failed ? ST_WAIT : finite ? 0 : ST_NONFINITE;
+            slot->status = gave_up ? ST_WAIT : finite ? 0 : ST_NONFINITE;
             *w.status = slot->status;
         }
-        if (failed) return;
+        if (gave_up) return;
         if (!finite) continue;
         __half* img = a.img + (int64_t)mat * a.mat_stride;
         for (int seg = a.parts - 1 - (a.parts - 1 - rank + g.team) % g.team; seg >= 0; seg -= g.team) {
@@ -300,15 +302,16 @@ __global__ void __launch_bounds__(BUFFER_THREADS, BUFFER_BLOCKS) buffer_kernel(c
 // A matrix goes through its products one after the other:
 //   group of one step    A = X X^T;  Q = a I + b A + c A^2;  X' = Q X
 //   group of two steps   A = X X^T;  Q = a I + b A + c A^2;  T = Q A;  A' = Q T;  Q' = a' I + b' A' + c' A'^2;  P = Q' Q;  X' = P X
-// (X in turns in two images; sq[0]: A and Q', sq[1]: Q, sq[2]: T and P, sq[3]: A').  The 256 x 256 tiles of one product of one matrix are
-// units of work; CTA pairs take the units of all matrices in turn, product after product.
+// (X in turns in two images; sq[0]: A and Q', sq[1]: Q, sq[2]: T and P, sq[3]: A').  The tiles of one product of one matrix are units of
+// work (of 256 x 256 for CTA pairs, or of 128 x 64 for single CTAs), which the pairs or CTAs take in turn, those of all matrices product
+// after product.
 //
 // Symmetric results.  All but X are polynomials of one symmetric matrix: tiles on and below the diagonal are computed and stored, and an operand
 // tile above it is read from its mirror image, along columns in place of rows (the MMA takes either).
 //
 // Order.  A unit loads a tile of an operand once its count has come to what the product that writes it leaves there, so the first units
 // of a product run beside the last ones of the product before.  A unit of product k stores its result when all units of product k - 2 are
-// done; no product writes what the one before reads.  Every unit waits for units in front of it only, and all pairs run at once.
+// done; no product writes what the one before reads.  Every unit waits for units in front of it only, and all CTAs run at once.
 // (One launch per product: 10 of 60 us of each between the last MMA of one and the first of the next for a 4096 x 4096 matrix, 6 of 10 for
 // 768 x 2048, and multiprocessors without work at the end of each.  One kernel that waits for whole products: 15 of 80 us, the results'
 // stores and their fences among them.)
@@ -416,7 +419,7 @@ __device__ __forceinline__ uint32_t writes_of(const Class& c, const Op& o, int i
     }
 }
 
-// A walk over the units of a launch, one pair's share.
+// A walk over the units of a launch: the share of one CTA (pair).
 struct Walk {
     int stage, cls, base;      // the (product, class) that `unit` is in, and its first unit
     int unit;

@@ -132,3 +132,79 @@ def test_binding_checks_tensors_before_pointers():
         od.orthdion_muon_set_schedule(od.orthdion_muon_create(8, 8, 0.9, 0.1, 0.0), [(1.0, 2.0)])
     with pytest.raises(ValueError):
         od.MuonTable([], [], [], [])
+
+
+class Fake:
+    """A CUDA tensor as far as the binding looks at one."""
+
+    def __init__(self, ptr, shape, dtype, device=0):
+        import torch
+        self.ptr, self.shape, self.dtype, self.device, self.is_cuda = ptr, tuple(shape), dtype, torch.device("cuda", device), True
+
+    def stride(self, k):
+        return (self.shape[1], 1)[k]
+
+    def numel(self):
+        n = 1
+        for s in self.shape:
+            n *= s
+        return n
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return self.ptr
+
+
+def test_tables_are_checked_again_before_a_call(L, monkeypatch):
+    """Plans that changed or went, and tensors of another device than the current one, are refused before a pointer is handed on."""
+    import torch
+    from paper_2605_16341_b200 import binding as od
+    current = [0]
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    monkeypatch.setattr(od, "_stream_ptr", lambda stream: 0)
+    bf, f32 = torch.bfloat16, torch.float32
+    h = od.orthdion_muon_create(64, 48, 0.9, 0.1, 0.0)
+    a = od.orthdion_adamw_create(100, 0.9, 0.95, 1e-8, 0.1, 0.0)
+    X, M, G = Fake(256, (64, 48), bf), Fake(1 << 20, (64, 48), f32), Fake(2 << 20, (64, 48), bf)
+    ws, off = Fake(3 << 20, (64,), torch.uint8), Fake(3 << 20, (64,), torch.uint8, 1)
+    table = od.MuonTable([h], [X], [M], [G])
+    with pytest.raises(od.OrthDionError) as e:          # as far as the library: the workspace is too small
+        od.orthdion_muon_step_grouped(table, ws)
+    assert e.value.code == -4
+    with pytest.raises(ValueError):
+        od.orthdion_muon_step_grouped(table, off)
+    v = [Fake(k << 20, (100,), d) for k, d in ((5, bf), (6, f32), (7, f32), (8, bf))]
+    step, far = Fake(9 << 20, (2,), torch.int64), Fake(9 << 20, (2,), torch.int64, 1)
+    adamw = od.AdamWTable([a], *[[t] for t in v])
+    with pytest.raises(ValueError):
+        od.orthdion_adamw_step_grouped(adamw, far)
+    current[0] = 1
+    for call in (lambda: od.orthdion_muon_step_grouped(table, off), lambda: od.orthdion_orthogonalize_grouped(table, off),
+                 lambda: od.orthdion_adamw_step_grouped(adamw, far), lambda: od.orthdion_muon_step(h, X, M, G, off)):
+        with pytest.raises(ValueError):
+            call()
+    current[0] = 0
+    for bad in (lambda: od.MuonTable([a], [X], [M], [G]), lambda: od.AdamWTable([h], *[[t] for t in v])):
+        with pytest.raises(od.OrthDionError):
+            bad()
+    od.orthdion_muon_set_dtypes(h, bf, f32)
+    od.orthdion_adamw_set_dtypes(a, f32, bf)
+    with pytest.raises(ValueError):
+        od.orthdion_muon_step_grouped(table, ws)
+    with pytest.raises(ValueError):
+        od.orthdion_adamw_step_grouped(adamw, step)
+    od.orthdion_muon_set_dtypes(h, bf, bf)
+    od.orthdion_muon_set_ld(h, 56, 48, 48)
+    with pytest.raises(ValueError):
+        od.orthdion_muon_step_grouped(table, ws)
+    od.orthdion_muon_destroy(h)
+    od.orthdion_adamw_destroy(a)
+    for call in (lambda: od.orthdion_muon_step_grouped(table, ws), lambda: od.orthdion_adamw_step_grouped(adamw, step)):
+        with pytest.raises(od.OrthDionError) as e:
+            call()
+        assert e.value.code == -1
