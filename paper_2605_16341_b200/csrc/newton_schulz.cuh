@@ -316,13 +316,14 @@ __global__ void __launch_bounds__(BUFFER_THREADS, BUFFER_BLOCKS) buffer_kernel(c
 // 768 x 2048, and multiprocessors without work at the end of each.  One kernel that waits for whole products: 15 of 80 us, the results'
 // stores and their fences among them.)
 constexpr int STAGE_RING = 196608;            // bytes of the operand ring
-// Three warpgroups: scout, producer and issuer (and a warp without work), and eight epilogue warps, which take most of the registers that the first
+// Three warpgroups: producer, issuer, scout and herald, and eight epilogue warps, which take most of the registers that the first
 // gives back: 128 x 80 + 256 x 208 of the 384 x 168 that the block is launched with.
 constexpr int THREADS = 384, FEW_REGS = 80, MANY_REGS = 208;
 static_assert(128 * FEW_REGS + 256 * MANY_REGS <= THREADS * 168, "registers");
 constexpr int MAX_STAGES = 8;
 constexpr int UNITS = 4;                      // that the scout is ahead of the epilogue at most
-constexpr int SMEM_BYTES = 1024 + STAGE_RING + 8 * 4096 + 256 + UNITS * 128;      // operands, epilogue blocks, barriers, units
+constexpr int BARRIERS = 384;                 // bytes
+constexpr int SMEM_BYTES = 1024 + STAGE_RING + 8 * 4096 + BARRIERS + UNITS * 128;      // operands, epilogue blocks, barriers, units
 // Two shapes of a tile.  PAIR: 256 x 256, two CTAs of 128 rows and 128 columns' operands each: 32 KB of operands (a plane) for 512 cycles of
 // MMAs, about what a multiprocessor takes in.  Else 128 x 64 of one CTA, 24 KB for 128 cycles: for calls of few tiles, whose
 // products then run on six times as many multiprocessors, and whose tiles leave six times as fast.
@@ -843,8 +844,9 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
     unsigned char* smem = smem_raw + (base - raw);
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + STAGE_RING + 8 * 4096);
     const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * MAX_STAGES, tfull0 = empty0 + 8 * MAX_STAGES, tempty0 = tfull0 + 16;
-    const uint32_t ufull0 = tempty0 + 16, uempty0 = ufull0 + 8 * UNITS;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * MAX_STAGES + 4 + 2 * UNITS);
+    const uint32_t ufull0 = tempty0 + 16, uempty0 = ufull0 + 8 * UNITS, udone0 = uempty0 + 8 * UNITS;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * MAX_STAGES + 4 + 3 * UNITS);
+    static_assert((2 * MAX_STAGES + 4 + 3 * UNITS) * 8 + 12 <= BARRIERS && BARRIERS % 128 == 0, "barriers");
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const uint32_t ready_at = smem_u32(tmem_slot + 2);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -852,7 +854,7 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
     if (threadIdx.x == 0) {
         for (int s = 0; s < NS; ++s) { mbar_init(full0 + 8 * s, SH::CTAS); mbar_init(empty0 + 8 * s, 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(tfull0 + 8 * a, 1); mbar_init(tempty0 + 8 * a, SH::ARRIVALS); }
-        for (int e = 0; e < UNITS; ++e) { mbar_init(ufull0 + 8 * e, 1); mbar_init(uempty0 + 8 * e, 8); }
+        for (int e = 0; e < UNITS; ++e) { mbar_init(ufull0 + 8 * e, 1); mbar_init(uempty0 + 8 * e, 1); mbar_init(udone0 + 8 * e, 8); }
         tmem_slot[2] = 0;
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -870,7 +872,7 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
     const uint32_t tmem_base = *tmem_slot;
     const uint32_t full_ld = PAIR ? map_to_rank(full0, 0) : full0, tempty_ld = PAIR ? map_to_rank(tempty0, 0) : tempty0;
     // The scout's units, each until the epilogue warps are through with it; and how many depth blocks of all units so far it has found there.
-    Unit* ring = reinterpret_cast<Unit*>(smem + STAGE_RING + 8 * 4096 + 256);
+    Unit* ring = reinterpret_cast<Unit*>(smem + STAGE_RING + 8 * 4096 + BARRIERS);
     static_assert(sizeof(Unit) <= 128, "units in shared memory");
     auto unit_at = [&](int e) { return reinterpret_cast<Unit*>(reinterpret_cast<unsigned char*>(ring) + e * 128); };
 
@@ -1022,6 +1024,30 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
             }
         }
         __syncwarp();
+    } else if (warp == 3) {
+        // ---------------- herald: tells of a unit when all epilogue warps are through with it ----------------
+        // (By each of those, with a fence behind its stores, this held it up for 1.5 to 3 us a unit: 28 matrices of 768 and 2048 took 496 us for
+        // 476, 768 x 2048 181 for 176.  Two planes, whose unit takes longer, have nothing of it: 256 x 512 140 for 142.)
+        if (lane == 0) {
+            int e = 0; uint32_t eph = 0;
+            while (mbar_wait(ufull0 + 8 * e, eph, abort_flag)) {
+                const Unit& u = *unit_at(e);
+                if (!u.kblocks || !mbar_wait(udone0 + 8 * e, eph, abort_flag)) break;
+                if (u.op.out >= 0 && !u.split) {
+                    const Class& c = g.c[u.cls];
+                    const int bj = u.tj / SH::Q;
+                    const int place = u.op.out < 4 ? u.op.out * c.blocks_sq + u.ti * (u.ti + 1) / 2 + bj
+                                                   : 4 * c.blocks_sq + (u.op.out - 4) * c.blocks_x + u.ti * SH::blocks(c.n) + bj;
+                    asm volatile("fence.proxy.async;" ::: "memory");
+                    asm volatile("fence.acq_rel.gpu;" ::: "memory");
+                    asm volatile("red.relaxed.gpu.global.add.u32 [%0], 8;" ::"l"(c.tile_done + (int64_t)u.mat * c.counts + place) : "memory");
+                    asm volatile("red.relaxed.gpu.global.add.u32 [%0], 8;" ::"l"(&c.slot[u.mat].done) : "memory");
+                }
+                mbar_arrive(uempty0 + 8 * e);
+                if (++e == UNITS) { e = 0; eph ^= 1; }
+            }
+        }
+        __syncwarp();
     } else if (warp >= 4) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(MANY_REGS));
         // ---------------- epilogue: warp w has the 32 rows that its tensor-memory quarter holds, and half the columns ----------------
@@ -1123,21 +1149,9 @@ __global__ void __launch_bounds__(THREADS, 1) chain_kernel(const __grid_constant
                 }
             }
             release();
-            if (u.op.out >= 0) {
-                // every lane's stores before the counts (which release them, by way of lane 0)
-                __syncwarp();
-                if (lane == 0 && !u.split) {
-                    const int bj = u.tj / SH::Q;
-                    const int place = u.op.out < 4 ? u.op.out * c.blocks_sq + u.ti * (u.ti + 1) / 2 + bj
-                                                   : 4 * c.blocks_sq + (u.op.out - 4) * c.blocks_x + u.ti * SH::blocks(c.n) + bj;
-                    asm volatile("fence.proxy.async;" ::: "memory");
-                    asm volatile("fence.acq_rel.gpu;" ::: "memory");
-                    asm volatile("red.relaxed.gpu.global.add.u32 [%0], 1;" ::"l"(c.tile_done + (int64_t)u.mat * c.counts + place) : "memory");
-                    asm volatile("red.relaxed.gpu.global.add.u32 [%0], 1;" ::"l"(&c.slot[u.mat].done) : "memory");
-                }
-            }
+            // every lane's stores before the herald's counts (which release them, by way of lane 0 and the barrier)
             __syncwarp();
-            if (lane == 0) mbar_arrive(uempty0 + 8 * e);
+            if (lane == 0) mbar_arrive(udone0 + 8 * e);
             if (++e == UNITS) { e = 0; eph ^= 1; }
         }
     }
