@@ -79,17 +79,19 @@ int terms_of(const orthdion_muon_plan* p) { return p->passes == 3 ? 2 : 1; }
 
 // Steps per product with X.  A pair of steps makes one Gram product of X (s^2 l multiply-adds by half), A^2 twice,
 // A' = Q A Q and P = Q' Q (five products of s^3 by half in all) and X = P X (s^2 l): 3 l + 5 s against 2 (3 l + s) of single
-// steps, in units of s^2 by half.  The rounding of A, relative to its norm, is multiplied by up to a^2 where a pair forms A', which counts
+// steps, in units of s^2 by half, with one product more in sequence.  So pairs pay where the matrix is long: singles and pairs, us, 2048 x 2048 356,
+// 382; sixteen of 768 x 768 338, 359; 800 x 1200 187, 196; 1500 x 3000 306, 308; 800 x 3000 209, 203; three of 2048 x 5632 987, 892; with two
+// terms 2048 x 2048 622, 669; 800 x 1200 313, 337; eight of 1000 x 2000 832, 776; three of 2048 x 5632 2719, 2389.
+// The rounding of A, relative to its norm, is multiplied by up to a^2 where a pair forms A', which counts
 // while some directions have grown and others have not: not in the first two steps (all singular values are small after the division by
 // the norm) and not in the last two, but in between (noise and 32 strong directions, 129 x 1000, error of the result by grouping of five steps:
-// 2,2,1 8.1e-3; 1,2,2 2.8e-3; singles 2.5e-3; 2,1,2 2.3e-3; 2,1,1,1 2.2e-3).  A pair in front costs a square matrix nothing and saves
-// a rounding of X; one at the end pays where the matrix is longer than wide.  None with two terms, which need no care, where the number of products
-// counts, which is one less without a pair: up to 512 rows (256 x 512: 17 products 143 us, 15 126).
+// 2,2,1 8.1e-3; 1,2,2 2.8e-3; singles 2.5e-3; 2,1,2 2.3e-3; 2,1,1,1 2.2e-3).  With two terms none up to 512 rows, where the number of
+// products counts (256 x 512: 17 products 143 us, 15 126).
 struct Groups { int32_t pair_first, pair_last; };
 Groups group_steps(const orthdion_muon_plan* p) {
     const int64_t s = std::min(p->m, p->n), l = std::max(p->m, p->n);
-    if (p->passes == 3 && s <= 512) return Groups{0, 0};
-    return Groups{p->pairable[0], p->steps >= 5 && 4 * l >= 5 * s && p->pairable[1]};
+    if (l < 2 * s || (p->passes == 3 && s <= 512)) return Groups{0, 0};
+    return Groups{p->pairable[0], p->steps >= 5 && p->pairable[1]};
 }
 
 // Tiles and square blocks of the products of one matrix, with tiles of CTA pairs or of single CTAs.

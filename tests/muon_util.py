@@ -53,11 +53,11 @@ def bound(B, schedule, passes, x_dtype, eps=1e-7, exact_input=False, pairs=(True
 
     eye = torch.eye(s, dtype=torch.float64, device=X.device)
     err = (0.0 if exact_input and passes == 1 else u * fro(X)) + 2.0 ** -23 * fro(X)      # the scale that is left is rounded too
-    # steps between two roundings of X: two in front, and two at the end of five or more where the matrix is longer than wide;
-    # one by one where a small matrix has two-term operands
-    singles = passes == 3 and s <= 512
+    # steps between two roundings of X: two in front, and two at the end of five or more, where the matrix is twice as long as wide;
+    # one by one elsewhere, and where a small matrix has two-term operands
+    singles = l < 2 * s or (passes == 3 and s <= 512)
     # (`pairs`: whether the factors of the first two steps, and of the last two, fit the images together)
-    k, pair_last = 0, pairs[1] and len(schedule) >= 5 and 4 * l >= 5 * s and not singles
+    k, pair_last = 0, pairs[1] and len(schedule) >= 5 and not singles
     while k < len(schedule):
         steps = schedule[k:k + (2 if (k == 0 and pairs[0] and not singles) or (pair_last and len(schedule) - k == 2) else 1)]
         A = X @ X.T

@@ -215,7 +215,7 @@ def test_more_plans_than_one_launch_takes():
 def test_steep_schedules(tail, passes):
     """Two steps whose factors together (20 and 7) are beyond what an image holds are taken one by one, in front of a pair or not."""
     steep = [(20.0, -50.0, 32.0), (7.0, -0.9, 0.024), (0.125, 0.0, 0.0)] + tail
-    for m, n in ((600, 800), (100, 260)):
+    for m, n in ((600, 1300), (100, 260), (260, 200)):
         G = gradient("spikes", m, n, 2, BF16)
         got = orth(G, F32, steep, passes=passes)
         assert rel(got, orthogonalise(G, steep)) <= bound(G, steep, passes, F32, exact_input=True, pairs=(False, True))
