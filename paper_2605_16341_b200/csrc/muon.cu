@@ -141,7 +141,7 @@ Scratch scratch_layout(const orthdion_muon_plan* p, int count) {
     c.tile_done = align_up(count * sizeof(ns::Slot), 256);
     c.front = c.tile_done + align_up((size_t)count * std::max(tiles_of(p, true).counts(), tiles_of(p, false).counts()) * 4, 256);
     size_t off = 0;
-    c.part = off; off += align_up((size_t)count * 2 * ns::MAX_PARTS * 8, 1024);
+    c.part = off; off += align_up((size_t)count * ns::MAX_PARTS * 8, 1024);
     c.split = off;
     const size_t pair_part = (size_t)tiles_of(p, true).sq * ns::Shape<true>::ROWS * ns::Shape<true>::COLS;
     const size_t single_part = (size_t)tiles_of(p, false).sq * ns::Shape<false>::ROWS * ns::Shape<false>::COLS;
@@ -252,7 +252,6 @@ void encode(ns::Class& c, int i, bool pair, const void* base, int64_t cols, int6
     }
 }
 
-int g_buffer_blocks[kMaxDevices] = {};    // blocks of the buffer kernel, likewise
 int g_at_once[kMaxDevices][2] = {};       // single CTAs and CTA pairs of the chain kernel that the device runs at once; written under ensure_attributes()'s lock
 
 int current_device() {
@@ -261,10 +260,13 @@ int current_device() {
 }
 
 // by whether there is momentum, the gradient's type and whether there are whole vectors
-void (*const kBufferKernels[8])(ns::Table, ns::BufferArgs) = {
-    ns::buffer_kernel<ns::Form<false, false, false>>, ns::buffer_kernel<ns::Form<true, false, false>>, ns::buffer_kernel<ns::Form<false, true, false>>,
-    ns::buffer_kernel<ns::Form<true, true, false>>,   ns::buffer_kernel<ns::Form<false, false, true>>, ns::buffer_kernel<ns::Form<true, false, true>>,
-    ns::buffer_kernel<ns::Form<false, true, true>>,   ns::buffer_kernel<ns::Form<true, true, true>>};
+using BufferKernel = void (*)(ns::Table, ns::BufferArgs);
+template <class F>
+constexpr BufferKernel kBufferKernelsOf[2] = {ns::norm_kernel<F>, ns::image_kernel<F>};
+const BufferKernel* const kBufferKernels[8] = {
+    kBufferKernelsOf<ns::Form<false, false, false>>, kBufferKernelsOf<ns::Form<true, false, false>>, kBufferKernelsOf<ns::Form<false, true, false>>,
+    kBufferKernelsOf<ns::Form<true, true, false>>,   kBufferKernelsOf<ns::Form<false, false, true>>, kBufferKernelsOf<ns::Form<true, false, true>>,
+    kBufferKernelsOf<ns::Form<false, true, true>>,   kBufferKernelsOf<ns::Form<true, true, true>>};
 
 // A launch whose blocks wait for one another: all of them run at once, or none.
 template <class... KArgs, class... Args>
@@ -288,11 +290,7 @@ void cooperative(void (*kernel)(KArgs...), int grid, int block, size_t smem, int
 void run_launch(const orthdion_muon_t* hs, const Launch& l, void* const* X, float* const* M, const void* const* G, bool update, char* ws,
                 char* scratch, cudaStream_t st) {
     std::unique_ptr<ns::ChainArgs> args(new ns::ChainArgs());
-    struct Buffer {
-        ns::BufferArgs args{};
-        int32_t most_parts = 1, least_parts = ns::MAX_PARTS;
-    };
-    std::unique_ptr<Buffer[]> buffers(new Buffer[4]);
+    std::unique_ptr<ns::BufferArgs[]> buffers(new ns::BufferArgs[4]());
     ns::Table all{};
     const int terms = terms_of(hs[l.classes[0][0]]), at_once = g_at_once[current_device()][l.pair];
     args->classes = (int32_t)l.classes.size();
@@ -342,9 +340,8 @@ void run_launch(const orthdion_muon_t* hs, const Launch& l, void* const* X, floa
         // rows on 16-byte boundaries, and whole vectors
         const bool vec = p->n % 8 == 0 && p->ld_g % 8 == 0 && (!update || p->ld_m % 4 == 0);
         const int form = 2 * (p->g_dtype == ORTHDION_DTYPE_BF16) + vec;
-        Buffer& bu = buffers[form];
-        ns::PrepArgs& a = bu.args.c[bu.args.classes++];
-        bu.args.matrices += c.count;
+        ns::BufferArgs& bu = buffers[form];
+        ns::PrepArgs& a = bu.c[bu.classes++];
         a.rows = p->m; a.cols = p->n; a.ld_g = p->ld_g; a.ld_m = p->ld_m;
         a.nesterov = p->nesterov;
         a.mu = (float)p->mu; a.rest = (float)(1.0 - p->mu);
@@ -355,25 +352,24 @@ void run_launch(const orthdion_muon_t* hs, const Launch& l, void* const* X, floa
         a.slot = c.slot;
         a.img = c.x[0];
         a.pitch = sc.x_pitch; a.term_stride = sc.x_term; a.mat_stride = sc.x_mat;
-        // four chunks a thread in a segment, more where there would be too many of them
+        // eight chunks a thread in a piece of a norm, more where there would be too many sums, and four in a piece of an image
         const int64_t chunks = ns::chunks_per_row(p->n, vec) * p->m;
-        a.seg = std::max<int64_t>(4 * ns::BUFFER_THREADS, (int64_t)align_up((chunks + ns::MAX_PARTS - 1) / ns::MAX_PARTS, ns::BUFFER_THREADS));
-        a.parts = (int32_t)((chunks + a.seg - 1) / a.seg);
-        bu.most_parts = std::max(bu.most_parts, a.parts);
-        bu.least_parts = std::min(bu.least_parts, a.parts);
+        a.seg[0] = std::max<int64_t>(8 * ns::BUFFER_THREADS, (int64_t)align_up((chunks + ns::MAX_PARTS - 1) / ns::MAX_PARTS, ns::BUFFER_THREADS));
+        a.seg[1] = std::max<int64_t>(4 * ns::BUFFER_THREADS, (int64_t)align_up((size_t)(chunks >> 18) + 1, ns::BUFFER_THREADS));
+        for (int k = 0; k < 2; ++k) {
+            a.parts[k] = (int32_t)((chunks + a.seg[k] - 1) / a.seg[k]);
+            a.before[k] = bu.pieces[k];
+            bu.pieces[k] += a.parts[k] * c.count;
+        }
     }
     if (engine_error()) return;
     if (cudaMemsetAsync(scratch, 0, l.front, st) != cudaSuccess) { engine_error() = LAUNCH_FAILED; return; }
-    for (int form = 0; form < 4; ++form) {
-        Buffer& bu = buffers[form];
-        if (!bu.args.classes) continue;
-        // As many teams as there are matrices, but of blocks enough that each has a segment of the smallest one.
-        const int blocks = g_buffer_blocks[current_device()], matrices = bu.args.matrices;
-        const int teams = std::max(1, std::min(matrices, blocks / bu.least_parts));
-        bu.args.team = std::min(bu.most_parts, blocks / teams);
-        cooperative(kBufferKernels[4 * update + form], teams * bu.args.team, ns::BUFFER_THREADS, 0, 1,
-                    prof::S_NS_BUFFER, st, all, bu.args);
-    }
+    overlap_launches() = true;
+    for (int form = 0; form < 4; ++form)
+        if (buffers[form].classes)
+            for (int k = 0; k < 2; ++k)
+                launch(kBufferKernels[4 * update + form][k], dim3((unsigned)buffers[form].pieces[k]), ns::BUFFER_THREADS, 0, 1, prof::S_NS_BUFFER, st,
+                       all, buffers[form]);
 
     int units = 0;                 // of the products with the most tiles
     for (int k = 0; k < args->classes; ++k) units += std::max(args->c[k].tiles_sq * args->c[k].splits, args->c[k].tiles_x) * args->c[k].count;
@@ -405,12 +401,6 @@ int ensure_attributes() {
         if (e == cudaSuccess && n < 1) e = cudaErrorInvalidConfiguration;
         g_at_once[dev][pair] = g_at_once[dev][pair] ? std::min(g_at_once[dev][pair], n) : n;
     };
-    int per_sm = 0;
-    for (auto* kernel : kBufferKernels) {
-        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, ns::BUFFER_THREADS, 0);
-        const int n = std::max(1, std::min(per_sm, ns::BUFFER_BLOCKS)) * sm_count();
-        g_buffer_blocks[dev] = g_buffer_blocks[dev] ? std::min(g_buffer_blocks[dev], n) : n;
-    }
     set(ns::chain_kernel<true, 1>, true);
     set(ns::chain_kernel<true, 2>, true);
     set(ns::chain_kernel<false, 1>, false);

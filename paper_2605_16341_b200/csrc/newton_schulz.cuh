@@ -45,7 +45,8 @@ struct Slot {
     float sigma;       // UNIT / (stored |X0| + stored eps): how much larger the normalised matrix is than the stored one
     int32_t status;
     uint32_t done;     // epilogue warps that have finished a tile of one of its products
-    uint32_t summed;   // blocks that have finished their share of the norm
+    uint32_t summed;   // pieces whose squares are summed
+    int32_t p2;        // power of two that B is stored times
 };
 
 // ---- the buffer B, its norm, its image ---------------------------------------------------------
@@ -55,9 +56,10 @@ struct PrepArgs {
     float mu, rest;              // momentum, 1 - momentum
     double eps;
     int32_t first, count;        // matrices of the table
-    int32_t terms, parts;
-    int64_t seg;                 // chunks of one partial sum (by the matrix's size alone: the same sums in whatever call it stands)
-    double* part;                // [matrix][2][MAX_PARTS]
+    int32_t terms;
+    int32_t before[2], parts[2]; // of norms and images: pieces of the classes in front of this one, and of a matrix
+    int64_t seg[2];              // chunks of one piece (by the matrix's size alone: the same sums in whatever call it stands)
+    double* part;                // [matrix][MAX_PARTS]
     Slot* slot;                  // cleared
     __half* img;
     int64_t pitch, term_stride, mat_stride;      // of the image, in elements
@@ -65,7 +67,7 @@ struct PrepArgs {
 // Chunks of 8 entries in a row (the last ones may lie beyond its end).
 __host__ __device__ inline int64_t chunks_per_row(int64_t cols, bool vec) { return vec ? (cols + 7) / 8 : (cols + 255) / 256 * 32; }
 struct BufferArgs {
-    int32_t classes, matrices, team;       // team: blocks that work on one matrix together
+    int32_t classes, pieces[2];
     PrepArgs c[MAX_CLASSES];
 };
 
@@ -122,15 +124,15 @@ __device__ __forceinline__ void buffer_of(const Raw<F>& r, const PrepArgs& a, fl
     }
 }
 
-constexpr int BUFFER_THREADS = 256, BUFFER_BLOCKS = 4;       // of a multiprocessor
-constexpr int BUFFER_U = 2;                                  // chunks under way in a thread
+constexpr int BUFFER_THREADS = 256;
+constexpr int BUFFER_U = 4;              // chunks under way in a thread (two: a layer of a 1.1B model 175 us, four 164, eight no less)
 
-// f(entries, row, column) for the chunks of segment `seg` that this thread takes, U of them loaded before the first is used.
+// f(entries, row, column) for the chunks of segment `seg` of `size` chunks that this thread takes, U of them loaded before the first is used.
 template <int U, class FORM, class F>
-__device__ __forceinline__ void for_chunks(const Mat& w, const PrepArgs& a, int seg, F f) {
-    const int64_t cpr = chunks_per_row(a.cols, FORM::VEC), begin = seg * a.seg, first = begin + threadIdx.x;
+__device__ __forceinline__ void for_chunks(const Mat& w, const PrepArgs& a, int64_t size, int seg, F f) {
+    const int64_t cpr = chunks_per_row(a.cols, FORM::VEC), begin = seg * size, first = begin + threadIdx.x;
     auto column = [](int c) { return FORM::VEC ? c * 8 : c / 32 * 256 + c % 32; };
-    int left = (int)min(a.seg, cpr * a.rows - begin) - (int)threadIdx.x;       // chunks from this thread's next one to the end
+    int left = (int)min(size, cpr * a.rows - begin) - (int)threadIdx.x;       // chunks from this thread's next one to the end
     const int width = (int)cpr, drow = BUFFER_THREADS / width, dc = BUFFER_THREADS - drow * width;
     int row = (int)(first / cpr), c = (int)(first - row * cpr);
     auto next = [&] {
@@ -169,27 +171,27 @@ __device__ __forceinline__ double block_sum(double v, double* red) {
     return v;
 }
 
-template <class FORM, bool WIDE>
+template <class FORM>
 __device__ __forceinline__ double sum_segment(const Mat& w, const PrepArgs& a, int seg) {
     double sum = 0.0;
-    for_chunks<FORM::VEC && !WIDE ? BUFFER_U : 1, FORM>(w, a, seg, [&](const Raw<FORM>& r, int, int) {
+    for_chunks<FORM::VEC ? BUFFER_U : 1, FORM>(w, a, a.seg[0], seg, [&](const Raw<FORM>& r, int, int) {
         float b[8], m[8];
         buffer_of<FORM>(r, a, b, m);
-        if (WIDE) {
+        float q = b[0] * b[0];                   // eight squares in 32 bits, in 64 where those overflow or may have vanished
+#pragma unroll
+        for (int e = 1; e < 8; ++e) q = fmaf(b[e], b[e], q);
+        if (q >= 1e-25f && q <= 1e37f) {
+            sum += (double)q;
+        } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum = fma((double)b[e], (double)b[e], sum);
-        } else {
-            float q = b[0] * b[0];                   // eight squares in 32 bits
-#pragma unroll
-            for (int e = 1; e < 8; ++e) q = fmaf(b[e], b[e], q);
-            sum += (double)q;
         }
     });
     return sum;
 }
 template <class FORM>
 __device__ __forceinline__ void write_segment(const Mat& w, const PrepArgs& a, int seg, __half* img, float f1, float f2) {
-    for_chunks<FORM::VEC ? BUFFER_U : 1, FORM>(w, a, seg, [&](const Raw<FORM>& r, int row, int col) {
+    for_chunks<FORM::VEC ? BUFFER_U : 1, FORM>(w, a, a.seg[1], seg, [&](const Raw<FORM>& r, int row, int col) {
         float b[8], m[8];
         buffer_of<FORM>(r, a, b, m);
         if (FORM::MOMENTUM) {
@@ -230,72 +232,67 @@ __device__ __forceinline__ void write_segment(const Mat& w, const PrepArgs& a, i
     });
 }
 
-// What is left of one matrix when the last block of its team has summed: the image of B, scaled by the power of two that brings its norm to
-// [128, 256) (a gradient in bf16 is then held exactly; what is left of the normalisation, sigma, goes into the factors of the first products), and
-// the updated momentum.  A matrix whose norm is not finite keeps its momentum.  The second look at B finds most of it in L2: a team
-// works on one matrix at a time and goes back over it the way it came.  (As two launches, norms of all matrices and then images, the seven
-// matrices of a layer of a 1.1B model took 225 us, 18 bytes an entry at 4.1 TB/s, for 187 now.)
+// The piece that a block works on: of which matrix of which class.
+template <int WHICH>
+__device__ __forceinline__ const PrepArgs& piece_of(const BufferArgs& g, int piece, int& mat, int& seg) {
+    int k = 0;
+    while (k + 1 < g.classes && piece >= g.c[k + 1].before[WHICH]) ++k;
+    piece -= g.c[k].before[WHICH];
+    mat = piece / g.c[k].parts[WHICH];
+    seg = piece - mat * g.c[k].parts[WHICH];
+    return g.c[k];
+}
+
+// Norms: a block per piece, and the one that is done last with a matrix adds up its sums, always in the same order.  Then images: a block per piece, from
+// the last one back, so that what was read last is still in L2.  Both are plain streams of one pass.  (As one kernel of teams of blocks per matrix,
+// which waited for the norm and looked at G and M again in L2, the seven matrices of a layer of a 1.1B model took 187 us for 164, 28 of a 320M model 111
+// for 103: reads and writes in turns.)
 template <class FORM>
-__global__ void __launch_bounds__(BUFFER_THREADS, BUFFER_BLOCKS) buffer_kernel(const __grid_constant__ Table t, const __grid_constant__ BufferArgs g) {
+__global__ void __launch_bounds__(BUFFER_THREADS) norm_kernel(const __grid_constant__ Table t, const __grid_constant__ BufferArgs g) {
     __shared__ double red[BUFFER_THREADS / 32];
-    __shared__ int failed;
+    __shared__ int last;
     grid_dependency();
-    const int rank = (int)blockIdx.x % g.team, teams = (int)gridDim.x / g.team;
-    int cls = 0, before = 0;
-    for (int k = (int)blockIdx.x / g.team; k < g.matrices; k += teams) {
-        while (k >= before + g.c[cls].count) before += g.c[cls++].count;
-        const PrepArgs& a = g.c[cls];
-        const int mat = k - before;
-        const Mat& w = t.w[a.first + mat];
-        Slot* slot = a.slot + mat;
-        double* part = a.part + (int64_t)mat * (2 * MAX_PARTS);
-        double sum = 0.0;
-        int gave_up = 0;
-        // Once with squares in 32 bits, eight at a time; where the sum says that some overflowed or most of it vanished, all in 64.
-        for (int wide = 0; wide < 2; ++wide) {
-            for (int seg = rank; seg < a.parts; seg += g.team) {
-                const double mine = wide ? sum_segment<FORM, true>(w, a, seg) : sum_segment<FORM, false>(w, a, seg);
-                const double all = block_sum(mine, red);
-                if (threadIdx.x == 0) __stcg(part + wide * MAX_PARTS + seg, all);
-            }
-            if (threadIdx.x == 0) {
-                const uint32_t want = (uint32_t)(g.team * (wide + 1));
-                uint32_t v = 0;
-                asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(&slot->summed) : "memory");
-                const long long t0 = clock64();
-                do {
-                    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(&slot->summed) : "memory");
-                } while ((int32_t)(v - want) < 0 && clock64() - t0 < WAIT_LIMIT_CYCLES);
-                failed = (int32_t)(v - want) < 0;
-            }
-            __syncthreads();
-            gave_up = failed;                // (before the next barrier: thread 0 may be at the next matrix soon after it)
-            sum = 0.0;
-#pragma unroll
-            for (int i = 0; i < MAX_PARTS; i += BUFFER_THREADS)
-                if (i + (int)threadIdx.x < a.parts) sum += __ldcg(part + wide * MAX_PARTS + i + threadIdx.x);
-            sum = block_sum(sum, red);
-            if (gave_up || (sum >= 1e-20 && sum <= 1.7e308)) break;
-        }
-        const double norm = sqrt(sum);
-        const bool finite = norm <= 1.7e308;
-        int e = 0;
-        if (finite && norm > 0.0) frexp(norm, &e);
-        const int p2 = finite && norm > 0.0 ? 8 - e : 0;
-        // (the power itself may be beyond fp32, so two factors)
-        const float f1 = ldexpf(1.f, p2 / 2), f2 = ldexpf(1.f, p2 - p2 / 2);
-        if (threadIdx.x == 0 && (rank == 0 || gave_up)) {
-            slot->sigma = finite && norm > 0.0 ? (float)((double)UNIT / ldexp(norm + a.eps, p2)) : 0.f;
-            slot->status = gave_up ? ST_WAIT : finite ? 0 : ST_NONFINITE;
-            *w.status = slot->status;
-        }
-        if (gave_up) return;
-        if (!finite) continue;
-        __half* img = a.img + (int64_t)mat * a.mat_stride;
-        for (int seg = a.parts - 1 - (a.parts - 1 - rank + g.team) % g.team; seg >= 0; seg -= g.team) {
-            write_segment<FORM>(w, a, seg, img, f1, f2);
-        }
+    int mat, seg;
+    const PrepArgs& a = piece_of<0>(g, (int)blockIdx.x, mat, seg);
+    const Mat& w = t.w[a.first + mat];
+    Slot* slot = a.slot + mat;
+    double* part = a.part + (int64_t)mat * MAX_PARTS;
+    double sum = block_sum(sum_segment<FORM>(w, a, seg), red);
+    if (threadIdx.x == 0) {
+        __stcg(part + seg, sum);
+        __threadfence();
+        last = atomicAdd(&slot->summed, 1u) + 1u == (uint32_t)a.parts[0];
     }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    sum = 0.0;
+    for (int i = threadIdx.x; i < a.parts[0]; i += BUFFER_THREADS) sum += __ldcg(part + i);
+    sum = block_sum(sum, red);
+    if (threadIdx.x == 0) {
+        // The image of B is scaled by the power of two that brings its norm to [128, 256) (a gradient in bf16 is then held exactly); what is left
+        // of the normalisation, sigma, goes into the factors of the first products.
+        const double norm = sqrt(sum);
+        const bool finite = norm <= 1.7e308, scaled = finite && norm > 0.0;
+        int e = 0;
+        if (scaled) frexp(norm, &e);
+        slot->p2 = scaled ? 8 - e : 0;
+        slot->sigma = scaled ? (float)((double)UNIT / ldexp(norm + a.eps, 8 - e)) : 0.f;
+        slot->status = finite ? 0 : ST_NONFINITE;
+        *w.status = slot->status;
+    }
+}
+// The image, and the updated momentum.  A matrix whose norm is not finite keeps its momentum.
+template <class FORM>
+__global__ void __launch_bounds__(BUFFER_THREADS) image_kernel(const __grid_constant__ Table t, const __grid_constant__ BufferArgs g) {
+    grid_dependency();
+    int mat, seg;
+    const PrepArgs& a = piece_of<1>(g, g.pieces[1] - 1 - (int)blockIdx.x, mat, seg);
+    const Slot* slot = a.slot + mat;
+    if (__ldcg(&slot->status)) return;
+    const int p2 = __ldcg(&slot->p2);
+    // (the power itself may be beyond fp32, so two factors)
+    write_segment<FORM>(t.w[a.first + mat], a, seg, a.img + (int64_t)mat * a.mat_stride, ldexpf(1.f, p2 / 2), ldexpf(1.f, p2 - p2 / 2));
 }
 
 // ---- the products: one persistent kernel for all steps of a batch ------------------------------------
