@@ -73,6 +73,14 @@ def test_magnitudes(factor):
     assert rel(orth(G, F32, [FAST] * 5, eps=0.0), ref) <= min(tol, STATED[3])
 
 
+@pytest.mark.parametrize("m,n", [(40, 104), (41, 103)])
+def test_one_entry_above_all_others(m, n):
+    # its square overflows 32 bits, the others' do not: rank one as far as fp32 can tell
+    G = gradient("noise", m, n, 4, F32)
+    G[3, 5] = 1e30
+    assert rel(orth(G, F32), orthogonalise(G, [FAST] * 5)) <= STATED[3]
+
+
 def test_zeros_stay_zeros_and_eps_counts():
     for eps in (0.0, 1e-7):
         assert orth(torch.zeros(70, 90, device="cuda"), F32, [FAST] * 5, eps=eps).abs().max().item() == 0.0
